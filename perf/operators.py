@@ -296,8 +296,8 @@ def _run_plain(s):
         logs = (z.gather(-1, at) - most) / T - total.log()
         out["loss"] = T * T * s["weight"] * (t * (logt - logs)).sum(-1)
         if op == "distill_loss":
-            none = torch.tensor([0.0, 1.0], device="cuda")     # of a token that takes no part
-            out["stats"] = torch.where(weight == 0, none, torch.cat([most, total], -1))
+            # zeros of a token that takes no part
+            out["stats"] = torch.where(weight == 0, 0.0, torch.cat([most, total], -1))
             return out
     dz = torch.zeros(s["z"].shape, dtype=torch.float32, device="cuda")
     dz[..., :V] = e / total
@@ -401,8 +401,7 @@ def _exact_distill(case, s):
             else:
                 most = z.max(-1, keepdim=True).values
                 total = ((z - most) / T).exp().sum(-1, keepdim=True)
-            stats[m, a:b] = torch.cat([most, total], -1)
-            stats[m, a:b][w[:, 0] == 0] = torch.tensor([0.0, 1.0], dtype=torch.float64, device="cuda")
+            stats[m, a:b] = torch.where(w == 0, 0.0, torch.cat([most, total], -1))
             logs = (z - most) / T - total.log()
             terms = t * (logt - logs.gather(1, idx.clamp(min=0)))
             loss[m, a:b] = T * T * (w * terms.masked_fill(idx < 0, 0.0)).sum(-1)
