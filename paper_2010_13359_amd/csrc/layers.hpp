@@ -1,0 +1,150 @@
+// Shared parts of the layer operators (include/dqgan_layers.h): argument
+// checks, access to activations of any type at any alignment, reductions over
+// a wave and a workgroup.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/dqgan_layers.h"
+#include "device.hpp"
+#include "plan.hpp"
+
+namespace dq {
+
+// ---------------------------------------------------------------------------
+// host: argument checks and dispatch
+
+#define DQ_TRY(expr)                   \
+    do {                               \
+        dqgan_status s_ = (expr);      \
+        if (s_ != DQGAN_OK) return s_; \
+    } while (0)
+
+constexpr int64_t kMaxRows = INT32_MAX;          // tokens of all workers together
+constexpr int64_t kMaxTokens = int64_t(1) << 30;
+constexpr int64_t kMaxWidth = int64_t(1) << 24;
+
+// A device pointer that the call uses if `used`.
+inline dqgan_status check_ptr(const void *p, bool used = true) {
+    if (!p) return used ? DQGAN_EINVAL : DQGAN_OK;
+    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 ? DQGAN_OK : DQGAN_EALIGN;
+}
+inline dqgan_status check_device(const dqgan_plan_s *P) {
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return DQGAN_EHIP;
+    return dev == P->device ? DQGAN_OK : DQGAN_EINVAL;
+}
+inline bool tokens_ok(const dqgan_plan_s *P, int64_t tokens) {
+    return tokens >= 0 && tokens <= kMaxTokens && tokens * P->desc.M <= kMaxRows;
+}
+inline bool ldp_ok(const dqgan_plan_s *P, int64_t ldp) { return ldp == 0 || ldp == P->desc.ld; }
+inline bool type_ok(int32_t t) { return t == DQGAN_F32 || t == DQGAN_BF16 || t == DQGAN_F16; }
+
+// f(T{}) with T the C++ type of a dqgan_type.
+template <typename F>
+void with_type(int32_t type, F &&f) {
+    if (type == DQGAN_F32)
+        f(float{});
+    else if (type == DQGAN_BF16)
+        f(__bf16{});
+    else
+        f(_Float16{});
+}
+
+inline dqgan_status launched() { return hipGetLastError() == hipSuccess ? DQGAN_OK : DQGAN_EHIP; }
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ---------------------------------------------------------------------------
+// device: eight elements of a row per lane.  A row starts wherever an odd
+// width or offset puts it, so vectors are aligned to their element only; the
+// hardware loads and stores those in one instruction too.
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+template <typename T>
+struct Vec8 {
+    typedef T type __attribute__((ext_vector_type(8)));
+    typedef T packed __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+};
+
+// p[0..8), of which n are there; the others come as `fill`.
+template <typename T>
+__device__ __forceinline__ f32x8 load8(const T *p, int64_t n, float fill = 0.0f) {
+    if (n >= 8) {
+        const typename Vec8<T>::type v = *reinterpret_cast<const typename Vec8<T>::packed *>(p);
+        return __builtin_convertvector(v, f32x8);
+    }
+    f32x8 f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? static_cast<float>(p[i]) : fill;
+    return f;
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int64_t n, f32x8 f) {
+    if (n >= 8) {
+        const typename Vec8<T>::type v = __builtin_convertvector(f, typename Vec8<T>::type);
+        *reinterpret_cast<typename Vec8<T>::packed *>(p) = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = static_cast<T>(f[i]);
+}
+
+// Sum and maximum over the 64 lanes, in every lane (DPP: within quads, rows of
+// 16, then across rows).  The order of the sum is fixed.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_or(float old, float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, x),
+                                                                 CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ float lane63(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x += dpp_or<0xB1, 0xF>(0.0f, x);   // lane ^ 1
+    x += dpp_or<0x4E, 0xF>(0.0f, x);   // lane ^ 2
+    x += dpp_or<0x141, 0xF>(0.0f, x);  // half row mirrored
+    x += dpp_or<0x140, 0xF>(0.0f, x);  // row mirrored: every lane has its row's sum
+    x += dpp_or<0x142, 0xA>(0.0f, x);  // row 0 into row 1, row 2 into row 3
+    x += dpp_or<0x143, 0xC>(0.0f, x);  // rows 0 and 1 into rows 2 and 3
+    return lane63(x);
+}
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, dpp_or<0xB1, 0xF>(x, x));
+    x = fmaxf(x, dpp_or<0x4E, 0xF>(x, x));
+    x = fmaxf(x, dpp_or<0x141, 0xF>(x, x));
+    x = fmaxf(x, dpp_or<0x140, 0xF>(x, x));
+    x = fmaxf(x, dpp_or<0x142, 0xA>(x, x));
+    x = fmaxf(x, dpp_or<0x143, 0xC>(x, x));
+    return lane63(x);
+}
+
+// Sum over the W waves of a workgroup, in every lane.  `slot` is W floats of
+// LDS that the next call does not use again (two slots in turn).
+template <int W>
+__device__ __forceinline__ float group_sum(float x, float *slot) {
+    x = wave_sum(x);
+    if (W == 1) return x;
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float s = slot[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) s += slot[w];
+    return s;
+}
+template <int W>
+__device__ __forceinline__ float group_max(float x, float *slot) {
+    x = wave_max(x);
+    if (W == 1) return x;
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float s = slot[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) s = fmaxf(s, slot[w]);
+    return s;
+}
+
+}  // namespace dq

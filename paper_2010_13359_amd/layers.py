@@ -1,0 +1,262 @@
+"""Python binding of the layer operators (``include/dqgan_layers.h``): an
+embedding, layer norm and distillation from a teacher's top logits for the M
+workers of a plan, whose parameters lie in the rows of the evaluation points
+and whose parameter gradients go into the rows of the gradients.
+
+As in ``dqgan``, torch tensors supply device memory and the stream, and every
+tensor is checked against the plan and the other tensors before the call;
+outputs and workspaces are the caller's.  Activations are float32, bfloat16 or
+float16, ``[M][tokens][width]`` and contiguous.
+"""
+import ctypes
+
+import torch
+
+from . import dqgan
+from .dqgan import F32, U32, _check, _ptr, _stream
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+INDEX_TYPES = {torch.int32: 0, torch.int64: 1}
+
+EXPORTS = ("dqgan_embed_forward", "dqgan_embed_bytes", "dqgan_embed_backward", "dqgan_norm_forward",
+           "dqgan_norm_bytes", "dqgan_norm_backward", "dqgan_distill_forward", "dqgan_distill_backward",
+           "dqgan_distill_fused", "dqgan_distill_bytes")
+
+
+class EmbedDesc(ctypes.Structure):
+    _fields_ = [("offset", ctypes.c_int64), ("vocab", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("tokens", ctypes.c_int64), ("scale", ctypes.c_float), ("type", ctypes.c_int32),
+                ("index_type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("gamma", ctypes.c_int64), ("beta", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("tokens", ctypes.c_int64), ("eps", ctypes.c_float), ("type", ctypes.c_int32),
+                ("reserved", ctypes.c_int64)]
+
+
+class DistillDesc(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int64), ("ld", ctypes.c_int64), ("tokens", ctypes.c_int64), ("k", ctypes.c_int32),
+                ("temperature", ctypes.c_float), ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+_lib = None
+
+
+def load():
+    """The built library, with the layer operators' argument types."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    L = dqgan.load()
+    P, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+    size = ctypes.POINTER(ctypes.c_size_t)
+    E, N, D = (ctypes.POINTER(x) for x in (EmbedDesc, NormDesc, DistillDesc))
+    L.dqgan_embed_forward.argtypes = [P, E, P, P, i64, P, P]
+    L.dqgan_embed_bytes.argtypes = [P, E, size]
+    L.dqgan_embed_backward.argtypes = [P, E, P, P, P, i32, P, P]
+    L.dqgan_norm_forward.argtypes = [P, N, P, P, i64, P, P, P]
+    L.dqgan_norm_bytes.argtypes = [P, N, size]
+    L.dqgan_norm_backward.argtypes = [P, N, P, P, P, i64, P, P, P, i32, P, P]
+    L.dqgan_distill_forward.argtypes = [P, D, P, P, P, P, P, P, P, P]
+    L.dqgan_distill_backward.argtypes = [P, D, P, P, P, P, P, P, P]
+    L.dqgan_distill_fused.argtypes = [P, D, P, P, P, P, P, P, P, P]
+    L.dqgan_distill_bytes.argtypes = [P, D, size]
+    for name in EXPORTS:
+        getattr(L, name).restype = i32
+    _lib = L
+    return L
+
+
+def _type(dtype, name):
+    if dtype not in TYPES:
+        raise TypeError("%s: dtype %s, expected one of %s" % (name, dtype, ", ".join(str(t) for t in TYPES)))
+    return TYPES[dtype]
+
+
+def _rows(plan, t, name, width=None):
+    """[M][tokens] or [M][tokens][width] of a tensor that says how many tokens a call has."""
+    dims = 2 if width is None else 3
+    if not isinstance(t, torch.Tensor) or t.dim() != dims or t.shape[0] != plan.M:
+        raise ValueError("%s: expected a tensor of [%d][tokens]%s" % (name, plan.M, "" if width is None else "[width]"))
+    return t.shape[1]
+
+
+def _like(plan, t, name, shape, dtypes):
+    """Device pointer of a tensor that has to have this shape."""
+    if t is None:
+        return None
+    p = _ptr(t, name, 0, dtypes, plan.device)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    return p or None
+
+
+def _params(plan, P):
+    """Pointer and row stride of parameters: [M][ld], one row per worker, or
+    one vector of ld that all workers read."""
+    if P is None:
+        return None, plan.ld
+    if isinstance(P, torch.Tensor) and P.dim() == 1 and plan.M > 1:
+        return plan._vec(P, "P"), 0
+    return plan._mat(P, "P"), plan.ld
+
+
+def _workspace(plan, t, need):
+    """Pointer of the caller's workspace: any contiguous tensor of enough bytes."""
+    if t is None and need:
+        raise ValueError("workspace: the call needs %d bytes" % need)
+    return _ptr(t, "workspace", need, None, plan.device) or None
+
+
+def _bytes(fn, plan, desc):
+    n = ctypes.c_size_t()
+    _check(fn, getattr(load(), fn)(plan.handle, ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def _new(plan, n):
+    return torch.empty(n, dtype=torch.uint8, device="cuda:%d" % plan.device) if n else None
+
+
+# ---------------------------------------------------------------------------
+# embedding
+
+
+def embed_forward(plan, tokens, P, out, vocab, offset=0, scale=1.0, stream=None):
+    """out[m][n] = scale * row tokens[m][n] of worker m's table, which lies at
+    `offset` of its row of P ([vocab][width]); 0 where the token is below 0 or
+    at or beyond vocab.  tokens int32 or int64 [M][tokens]; P [M][ld], or [ld]
+    for all workers; out [M][tokens][width]."""
+    n = _rows(plan, out, "out", True)
+    d = EmbedDesc(offset, vocab, out.shape[2], n, scale, _type(out.dtype, "out"), 0, 0)
+    tok = _like(plan, tokens, "tokens", (plan.M, n), tuple(INDEX_TYPES))
+    d.index_type = INDEX_TYPES.get(getattr(tokens, "dtype", None), 0)
+    p, ldp = _params(plan, P)
+    _check("dqgan_embed_forward", load().dqgan_embed_forward(plan.handle, ctypes.byref(d), tok, p, ldp,
+                                                             _like(plan, out, "out", out.shape, tuple(TYPES)),
+                                                             _stream(stream)))
+
+
+def embed_workspace(plan, tokens, vocab, width, dtype, index_dtype=torch.int64, offset=0):
+    """A workspace for embed_backward with up to `tokens` tokens per worker."""
+    d = EmbedDesc(offset, vocab, width, tokens, 1.0, _type(dtype, "dtype"), INDEX_TYPES[index_dtype], 0)
+    return _new(plan, _bytes("dqgan_embed_bytes", plan, d))
+
+
+def embed_backward(plan, tokens, dout, G, vocab, workspace, offset=0, scale=1.0, add=False, stream=None):
+    """The table's part of G [M][ld]: row v is scale * the sum of dout over the
+    tokens that are v, 0 for those that do not occur; with `add` the sums are
+    added to what is there."""
+    n = _rows(plan, dout, "dout", True)
+    d = EmbedDesc(offset, vocab, dout.shape[2], n, scale, _type(dout.dtype, "dout"), 0, 0)
+    tok = _like(plan, tokens, "tokens", (plan.M, n), tuple(INDEX_TYPES))
+    d.index_type = INDEX_TYPES.get(getattr(tokens, "dtype", None), 0)
+    ws = _workspace(plan, workspace, _bytes("dqgan_embed_bytes", plan, d))
+    _check("dqgan_embed_backward", load().dqgan_embed_backward(plan.handle, ctypes.byref(d), tok,
+                                                               _like(plan, dout, "dout", dout.shape, tuple(TYPES)),
+                                                               plan._mat(G, "G"), int(add), ws, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# layer norm
+
+
+def _norm_desc(plan, x, gamma, beta, eps):
+    n = _rows(plan, x, "x", True)
+    return NormDesc(-1 if gamma is None else gamma, -1 if beta is None else beta, x.shape[2], n, eps,
+                    _type(x.dtype, "x"), 0)
+
+
+def norm_forward(plan, x, P, y, stats=None, gamma=0, beta=None, eps=1e-5, stream=None):
+    """y = (x - mean) * rstd * weight + bias over the last dimension; weight and
+    bias at `gamma` and `beta` of each worker's row of P (None: without).
+    stats [M][tokens][2] float32 takes mean and rstd for norm_backward; y may
+    be x."""
+    d = _norm_desc(plan, x, gamma, beta, eps)
+    p, ldp = _params(plan, P)
+    same = (x.dtype,)
+    _check("dqgan_norm_forward",
+           load().dqgan_norm_forward(plan.handle, ctypes.byref(d), _like(plan, x, "x", x.shape, same), p, ldp,
+                                     _like(plan, y, "y", x.shape, same),
+                                     _like(plan, stats, "stats", x.shape[:2] + (2,), F32), _stream(stream)))
+
+
+def norm_workspace(plan, tokens, width, dtype, gamma=0, beta=None):
+    """A workspace for norm_backward of these sizes (None if it needs none)."""
+    d = NormDesc(-1 if gamma is None else gamma, -1 if beta is None else beta, width, tokens, 0.0,
+                 _type(dtype, "dtype"), 0)
+    return _new(plan, _bytes("dqgan_norm_bytes", plan, d))
+
+
+def norm_backward(plan, x, dy, P, stats, dx, G, workspace, gamma=0, beta=None, add=False, stream=None):
+    """dx (None: not wanted; it may be dy), and the sums over a worker's tokens
+    of dy * (x - mean) * rstd and of dy into its row of G at `gamma` and
+    `beta`; with `add` added to what is there."""
+    d = _norm_desc(plan, x, gamma, beta, 0.0)
+    p, ldp = _params(plan, P)
+    same = (x.dtype,)
+    ws = _workspace(plan, workspace, _bytes("dqgan_norm_bytes", plan, d))
+    _check("dqgan_norm_backward",
+           load().dqgan_norm_backward(plan.handle, ctypes.byref(d), _like(plan, x, "x", x.shape, same),
+                                      _like(plan, dy, "dy", x.shape, same), p, ldp,
+                                      _like(plan, stats, "stats", x.shape[:2] + (2,), F32),
+                                      _like(plan, dx, "dx", x.shape, same), plan._mat(G, "G"), int(add), ws,
+                                      _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# distillation
+
+
+def _distill(plan, z, val, idx, weight, vocab, temperature):
+    """Descriptor and the pointers that every form of the loss takes."""
+    n = _rows(plan, z, "z", True)
+    if not isinstance(val, torch.Tensor) or val.dim() != 3:
+        raise ValueError("val: expected a tensor of [%d][%d][k]" % (plan.M, n))
+    k = val.shape[2]
+    d = DistillDesc(z.shape[2] if vocab is None else vocab, z.shape[2], n, k, temperature, _type(z.dtype, "z"), 0)
+    return d, (_like(plan, z, "z", z.shape, tuple(TYPES)), _like(plan, val, "val", (plan.M, n, k), F32),
+               _like(plan, idx, "idx", (plan.M, n, k), U32), _like(plan, weight, "weight", (plan.M, n), F32))
+
+
+def distill_workspace(plan, tokens, vocab, k, dtype, ld=None):
+    """A workspace for distill_forward and distill_fused of these sizes (None
+    if they need none)."""
+    d = DistillDesc(vocab, vocab if ld is None else ld, tokens, k, 1.0, _type(dtype, "dtype"), 0)
+    return _new(plan, _bytes("dqgan_distill_bytes", plan, d))
+
+
+def distill_forward(plan, z, val, idx, weight, loss, stats, vocab=None, workspace=None, temperature=1.0, stream=None):
+    """loss [M][tokens] of student logits z [M][tokens][ld] (columns from vocab
+    on are padding) against softmax(val / T) over the teacher's entries val,
+    idx [M][tokens][k] (indices at or beyond vocab, as -1, are skipped):
+    weight * T^2 * KL; weight [M][tokens] or None.  stats [M][tokens][2] is
+    what distill_backward takes."""
+    d, args = _distill(plan, z, val, idx, weight, vocab, temperature)
+    rows = tuple(z.shape[:2])
+    ws = _workspace(plan, workspace, _bytes("dqgan_distill_bytes", plan, d))
+    _check("dqgan_distill_forward",
+           load().dqgan_distill_forward(plan.handle, ctypes.byref(d), *args, _like(plan, loss, "loss", rows, F32),
+                                        _like(plan, stats, "stats", rows + (2,), F32), ws, _stream(stream)))
+
+
+def distill_backward(plan, z, val, idx, weight, stats, dz, vocab=None, temperature=1.0, stream=None):
+    """dz of distill_forward's loss; `weight` times the gradient that each loss
+    receives takes its place as `weight`.  dz may be z."""
+    d, args = _distill(plan, z, val, idx, weight, vocab, temperature)
+    _check("dqgan_distill_backward",
+           load().dqgan_distill_backward(plan.handle, ctypes.byref(d), *args,
+                                         _like(plan, stats, "stats", tuple(z.shape[:2]) + (2,), F32),
+                                         _like(plan, dz, "dz", z.shape, (z.dtype,)), _stream(stream)))
+
+
+def distill_fused(plan, z, val, idx, weight, loss, dz, vocab=None, workspace=None, temperature=1.0, stream=None):
+    """distill_forward and distill_backward in one call, the same bits; dz may
+    be z."""
+    d, args = _distill(plan, z, val, idx, weight, vocab, temperature)
+    ws = _workspace(plan, workspace, _bytes("dqgan_distill_bytes", plan, d))
+    _check("dqgan_distill_fused",
+           load().dqgan_distill_fused(plan.handle, ctypes.byref(d), *args,
+                                      _like(plan, loss, "loss", tuple(z.shape[:2]), F32),
+                                      _like(plan, dz, "dz", z.shape, (z.dtype,)), ws, _stream(stream)))

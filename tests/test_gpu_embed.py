@@ -1,0 +1,162 @@
+"""Embedding lookup and its gradient against 64 bits: types of activations and
+tokens, odd widths and offsets, token counts on both sides of a chunk and a
+wave, tokens that all are the same, padded or out of range, and the parts of a
+row that are not the table's."""
+import pytest
+
+import layer_refs as ref
+
+pytestmark = pytest.mark.gpu
+
+# M, tokens, vocabulary, width, offset
+SHAPES = [(1, 1, 1, 1, 0), (3, 1, 5, 7, 1), (2, 31, 2, 8, 4), (1, 32, 3, 9, 2), (2, 33, 40, 512, 0), (1, 64, 511, 513, 3),
+          (3, 65, 512, 64, 7), (1, 300, 513, 1, 0), (2, 1000, 37, 100, 5), (1, 1025, 70000, 17, 0), (2, 2500, 300, 1030, 9),
+          (1, 5000, 4, 520, 0), (5, 0, 10, 12, 2)]
+
+
+def _tokens(kind, M, N, V, dtype, gen):
+    import torch
+    t = torch.randint(0, V, (M, N), generator=gen)
+    if kind == "zipf":
+        t = (torch.rand((M, N), generator=gen) ** 4 * V).long().clamp(max=V - 1)
+        t[torch.rand((M, N), generator=gen) < 0.1] = -1
+        t[torch.rand((M, N), generator=gen) < 0.05] = V
+    elif kind == "same":
+        t[:] = V - 1
+    elif kind == "padded":
+        t[:] = torch.tensor([-1, V, torch.iinfo(dtype).min, torch.iinfo(dtype).max])[
+            torch.randint(0, 4, (M, N), generator=gen)]
+    return t.to(dtype).cuda()
+
+
+def _setup(shape, kind, index, seed=0):
+    import torch
+    M, N, V, D, off = shape
+    gen = torch.Generator().manual_seed(seed)
+    pl = ref.plan(off + V * D + 3, M)
+    P = torch.randn((M, pl.ld), generator=gen).cuda()
+    return pl, P, _tokens(kind, M, N, V, getattr(torch, index), gen), gen
+
+
+@pytest.mark.parametrize("dt", sorted(ref.TYPES))
+@pytest.mark.parametrize("index", ["int32", "int64"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward(shape, index, dt):
+    import torch
+    from paper_2010_13359_amd import layers
+    M, N, V, D, off = shape
+    pl, P, t, _ = _setup(shape, "zipf", index)
+    out = torch.full((M, N, D), float("nan"), dtype=ref.TYPES[dt], device="cuda")
+    layers.embed_forward(pl, t, P, out, V, offset=off, scale=1.7)
+    for m in range(M):
+        want, err = ref.embed_forward(t[m], P[m, off:off + V * D].view(V, D), 1.7)
+        ref.check("out", out[m], want, err)
+    # one vector for all workers
+    layers.embed_forward(pl, t, P[0].clone(), out, V, offset=off, scale=-0.5)
+    for m in range(M):
+        want, err = ref.embed_forward(t[m], P[0, off:off + V * D].view(V, D), -0.5)
+        ref.check("out of one vector", out[m], want, err)
+    pl.close()
+
+
+@pytest.mark.parametrize("kind", ["zipf", "same", "padded", "uniform"])
+@pytest.mark.parametrize("dt", sorted(ref.TYPES))
+@pytest.mark.parametrize("shape", SHAPES)
+def test_backward(shape, dt, kind):
+    import torch
+    from paper_2010_13359_amd import layers
+    M, N, V, D, off = shape
+    pl, _, t, gen = _setup(shape, kind, "int64" if N % 2 else "int32", seed=N)
+    dout = torch.randn((M, N, D), generator=gen).to(ref.TYPES[dt]).cuda()
+    G = torch.randn((M, pl.ld), generator=gen).cuda()
+    before = G.clone()
+    ws = layers.embed_workspace(pl, N, V, D, dout.dtype, t.dtype, offset=off)
+    if ws is not None:
+        ws.fill_(0xFF)     # nothing in it is read before it is written
+    layers.embed_backward(pl, t, dout, G, V, ws, offset=off, scale=0.3)
+    first = G.clone()
+    layers.embed_backward(pl, t, dout, G, V, ws, offset=off, scale=2.0, add=True)
+    for m in range(M):
+        want, err = ref.embed_backward(t[m], dout[m], V, 0.3)
+        ref.check("G", first[m, off:off + V * D].view(V, D), want, err)
+        want, err = ref.embed_backward(t[m], dout[m], V, 2.0, first[m, off:off + V * D].view(V, D))
+        ref.check("G added to", G[m, off:off + V * D].view(V, D), want, err)
+    for x in (first, G):
+        assert torch.equal(x[:, :off], before[:, :off]) and torch.equal(x[:, off + V * D:], before[:, off + V * D:])
+    # equal calls, equal bits
+    again = before.clone()
+    layers.embed_backward(pl, t, dout, again, V, ws, offset=off, scale=0.3)
+    assert torch.equal(again.view(torch.int32), first.view(torch.int32))
+    pl.close()
+
+
+def test_gradient_is_the_lookups():
+    """The lookup is linear in the table: <dout, out(P + h E) - out(P)> is h times
+    <gradient, E> for every E, up to the roundings of three sums."""
+    import torch
+    from paper_2010_13359_amd import layers
+    shape = (2, 77, 19, 24, 5)
+    M, N, V, D, off = shape
+    pl, P, t, gen = _setup(shape, "zipf", "int64", seed=3)
+    E, dout = torch.randn(P.shape, generator=gen).cuda(), torch.randn((M, N, D), generator=gen).cuda()
+    G = torch.zeros_like(P)
+    layers.embed_backward(pl, t, dout, G, V, layers.embed_workspace(pl, N, V, D, dout.dtype, offset=off), offset=off,
+                          scale=1.5)
+    a, b = torch.empty_like(dout), torch.empty_like(dout)
+    h = 0.25
+    layers.embed_forward(pl, t, P, a, V, offset=off, scale=1.5)
+    layers.embed_forward(pl, t, P + h * E, b, V, offset=off, scale=1.5)
+    left = ((b.double() - a.double()) * dout.double()).sum() / h
+    right = (G.double() * E.double()).sum()
+    # each out is off by 1.5 (|P| + h|E|) times two roundings, the gradient by N + 2 roundings of its terms
+    size = float(((a.abs() + b.abs()) * dout.abs()).double().sum()) / h + float((G.abs() * E.abs()).double().sum()) * N
+    assert abs(float(left - right)) <= 4 * ref.U * size
+    pl.close()
+
+
+def test_nonfinite_gradients_stay_in_their_rows():
+    import torch
+    from paper_2010_13359_amd import layers
+    M, N, V, D = 1, 100, 9, 20
+    pl = ref.plan(V * D, M)
+    t = (torch.arange(N) % V)[None].cuda()
+    t[0, 50] = -1
+    dout = torch.ones((M, N, D), dtype=torch.bfloat16, device="cuda")
+    dout[0, 50] = float("nan")      # of a padded place: nowhere
+    dout[0, 3, 4] = float("inf")
+    dout[0, 7, 5] = float("nan")
+    G = torch.zeros((M, pl.ld), device="cuda")
+    layers.embed_backward(pl, t, dout, G, V, layers.embed_workspace(pl, N, V, D, dout.dtype))
+    bad = (~torch.isfinite(G)).nonzero().tolist()
+    assert bad == [[0, 3 * D + 4], [0, 7 * D + 5]]
+    pl.close()
+
+
+def test_tables_beyond_32_bits():
+    """A table of more than 2^31 elements: its last rows."""
+    import torch
+    from paper_2010_13359_amd import layers
+    V, D, off = 2_100_003, 1031, 3
+    print("table of", V * D, "elements", flush=True)
+    pl = ref.plan(off + V * D, 1)
+    P = torch.zeros((1, pl.ld), device="cuda")
+    t = torch.tensor([[V - 1, 0, V - 2, V, V - 1, 2_090_000]], device="cuda")
+    rows = torch.randn((t.shape[1], D), device="cuda")
+    for i, v in enumerate(t[0].tolist()):
+        if v < V:
+            P[0, off + v * D:off + (v + 1) * D] = rows[i]
+    out = torch.empty((1, t.shape[1], D), device="cuda")
+    layers.embed_forward(pl, t, P, out, V, offset=off)
+    rows[0], rows[3] = rows[4], 0.0
+    assert torch.equal(out[0], rows)
+    G = P.fill_(7.0)
+    dout = torch.randn_like(out)
+    layers.embed_backward(pl, t, dout, G, V, layers.embed_workspace(pl, t.shape[1], V, D, dout.dtype, offset=off),
+                          offset=off)
+    table = G[0, off:off + V * D].view(V, D)
+    assert torch.equal(table[V - 1], dout[0, 0] + dout[0, 4])
+    for i in (1, 2, 5):
+        assert torch.equal(table[int(t[0, i])], dout[0, i])
+    assert int(torch.count_nonzero(table.any(1))) == 4
+    assert bool((G[0, :off] == 7.0).all()) and bool((G[0, off + V * D:] == 7.0).all())
+    pl.close()

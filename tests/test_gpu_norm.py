@@ -1,0 +1,180 @@
+"""Layer norm and its gradients against 64 bits: widths on both sides of every
+row shape, odd offsets, rows of one value, far from zero, or with infinities
+and NaN; calls in place and without weight, bias, input gradient or tokens."""
+import pytest
+
+import layer_refs as ref
+
+pytestmark = pytest.mark.gpu
+
+WIDTHS = [1, 2, 7, 8, 9, 63, 64, 65, 300, 511, 512, 513, 1000, 1023, 1024, 1025, 2047, 2048, 2049, 4095, 4096, 4097, 8192,
+          8193, 16384, 16385, 32768, 32769, 40001]
+
+
+def _setup(M, N, D, dt, gamma, beta, seed=0, kind="normal"):
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    pl = ref.plan(2 * D + 20, M)
+    x = torch.randn((M, N, D), generator=gen)
+    if kind == "far":
+        x = x * 0.5 + 100.0
+    elif kind == "scales":
+        x = x * torch.exp(4 * torch.randn((M, N, 1), generator=gen))
+    elif kind == "equal":
+        x = torch.randn((M, N, 1), generator=gen).expand(M, N, D)
+    P = torch.randn((M, pl.ld), generator=gen)
+    return pl, x.contiguous().to(ref.TYPES[dt]).cuda(), P.cuda(), gen
+
+
+def _cut(P, m, at, D):
+    return None if at is None else P[m, at:at + D]
+
+
+@pytest.mark.parametrize("dt", sorted(ref.TYPES))
+@pytest.mark.parametrize("D", WIDTHS)
+def test_forward(D, dt):
+    import torch
+    from paper_2010_13359_amd import layers
+    for M, N, gamma, beta, kind in [(2, 9, 3, D + 5, "normal"), (1, 1, D + 11, None, "scales"), (3, 5, None, 1, "far"),
+                                    (1, 3, None, None, "equal")]:
+        pl, x, P, _ = _setup(M, N, D, dt, gamma, beta, seed=D + N, kind=kind)
+        y = torch.full_like(x, float("nan"))
+        stats = torch.full((M, N, 2), float("nan"), device="cuda")
+        layers.norm_forward(pl, x, P, y, stats, gamma=gamma, beta=beta, eps=1e-3)
+        for m in range(M):
+            w = ref.norm_forward(x[m], _cut(P, m, gamma, D), _cut(P, m, beta, D), 1e-3)
+            ref.check("y", y[m], w[0], w[1])
+            ref.check("mean", stats[m, :, 0], w[2], w[3])
+            ref.check("rstd", stats[m, :, 1], w[4], w[5])
+        # one vector for all workers, no statistics, in place
+        z = x.clone()
+        layers.norm_forward(pl, z, P[0].clone(), z, gamma=gamma, beta=beta, eps=1e-3)
+        for m in range(M):
+            w = ref.norm_forward(x[m], _cut(P, 0, gamma, D), _cut(P, 0, beta, D), 1e-3)
+            ref.check("y in place", z[m], w[0], w[1])
+        pl.close()
+
+
+@pytest.mark.parametrize("dt", sorted(ref.TYPES))
+@pytest.mark.parametrize("D", WIDTHS)
+def test_backward(D, dt):
+    import torch
+    from paper_2010_13359_amd import layers
+    for M, N, gamma, beta, kind in [(2, 37, 3, D + 5, "scales"), (1, 1, D + 11, None, "far"), (3, 5, None, 1, "normal"),
+                                    (1, 3, None, None, "normal"), (1, 130, 0, D, "normal")]:
+        pl, x, P, gen = _setup(M, N, D, dt, gamma, beta, seed=D + N, kind=kind)
+        dy = torch.randn(x.shape, generator=gen).to(x.dtype).cuda()
+        xd = x.double()
+        stats = torch.stack([xd.mean(-1), 1 / (xd.var(-1, correction=0) + 1e-3).sqrt()], -1).float()
+        G = torch.randn((M, pl.ld), generator=gen).cuda()
+        before = G.clone()
+        ws = layers.norm_workspace(pl, N, D, x.dtype, gamma=gamma, beta=beta)
+        assert (ws is None) == (gamma is None and beta is None)
+        if ws is not None:
+            ws.fill_(0xFF)
+        dx = torch.full_like(x, float("nan"))
+        layers.norm_backward(pl, x, dy, P, stats, dx, G, ws, gamma=gamma, beta=beta)
+        first = G.clone()
+        # added to, in place
+        dz = dy.clone()
+        layers.norm_backward(pl, x, dz, P, stats, dz, G, ws, gamma=gamma, beta=beta, add=True)
+        assert torch.equal(dz.view(torch.uint8), dx.view(torch.uint8))
+        own = torch.zeros(pl.ld, dtype=torch.bool, device="cuda")
+        for m in range(M):
+            w = ref.norm_backward(x[m], dy[m], _cut(P, m, gamma, D), stats[m])
+            ref.check("dx", dx[m], w[0], w[1])
+            for at, sums, err in ((gamma, w[2], w[3]), (beta, w[4], w[5])):
+                if at is None:
+                    continue
+                own[at:at + D] = True
+                ref.check("G", first[m, at:at + D], sums, err)
+                ref.check("G added to", G[m, at:at + D], sums + first[m, at:at + D].double().cpu(), err)
+        assert torch.equal(first[:, ~own], before[:, ~own]) and torch.equal(G[:, ~own], before[:, ~own])
+        # parameters only
+        if ws is not None:
+            layers.norm_backward(pl, x, dy, P, stats, None, G, ws, gamma=gamma, beta=beta)
+            assert torch.equal(G.view(torch.int32), first.view(torch.int32))
+        pl.close()
+
+
+def test_many_rows():
+    """More rows than workgroups, several workers."""
+    import torch
+    from paper_2010_13359_amd import layers
+    for M, N, D in [(3, 9001, 48), (2, 5003, 700), (1, 20011, 130)]:
+        pl, x, P, gen = _setup(M, N, D, "f16", 0, D, seed=1)
+        dy = torch.randn(x.shape, generator=gen).to(x.dtype).cuda()
+        y, dx, stats = torch.empty_like(x), torch.empty_like(x), torch.empty((M, N, 2), device="cuda")
+        layers.norm_forward(pl, x, P, y, stats, gamma=0, beta=D)
+        G = torch.zeros_like(P)
+        layers.norm_backward(pl, x, dy, P, stats, dx, G, layers.norm_workspace(pl, N, D, x.dtype, 0, D), gamma=0, beta=D)
+        for m in range(M):
+            w = ref.norm_forward(x[m], P[m, :D], P[m, D:2 * D], 1e-5)
+            ref.check("y", y[m], w[0], w[1])
+            w = ref.norm_backward(x[m], dy[m], P[m, :D], stats[m])
+            ref.check("dx", dx[m], w[0], w[1])
+            ref.check("dgamma", G[m, :D], w[2], w[3])
+            ref.check("dbeta", G[m, D:2 * D], w[4], w[5])
+        pl.close()
+
+
+def test_no_tokens():
+    import torch
+    from paper_2010_13359_amd import layers
+    pl, x, P, _ = _setup(2, 0, 12, "bf16", 0, 12)
+    G = torch.ones_like(P)
+    stats = torch.empty((2, 0, 2), device="cuda")
+    layers.norm_forward(pl, x, P, x, stats, gamma=0, beta=12)
+    ws = layers.norm_workspace(pl, 0, 12, x.dtype, 0, 12)
+    layers.norm_backward(pl, x, x, P, stats, None, G, ws, gamma=0, beta=12, add=True)
+    assert bool((G == 1).all())
+    layers.norm_backward(pl, x, x, P, stats, None, G, ws, gamma=0, beta=14)
+    assert bool((G[:, :12] == 0).all() and (G[:, 14:26] == 0).all() and (G[:, 12:14] == 1).all() and (G[:, 26:] == 1).all())
+    pl.close()
+
+
+def test_nonfinite_rows_stay_apart():
+    import torch
+    from paper_2010_13359_amd import layers
+    for D in (40, 700, 3000, 33000):
+        pl, x, P, gen = _setup(1, 9, D, "f32", 0, D)
+        clean = x.clone()
+        x[0, 2, 5], x[0, 4, 0], x[0, 6, D - 1] = float("nan"), float("inf"), -float("inf")
+        y, stats = torch.empty_like(x), torch.empty((1, 9, 2), device="cuda")
+        layers.norm_forward(pl, x, P, y, stats, gamma=0, beta=D)
+        good = [0, 1, 3, 5, 7, 8]
+        w = ref.norm_forward(clean[0], P[0, :D], P[0, D:2 * D], 1e-5)
+        ref.check("y", y[0, good], w[0][good], w[1][good])
+        assert bool(torch.isnan(y[0, [2, 4, 6]]).any(1).all())
+        dx, G, dy = torch.empty_like(x), torch.zeros_like(P), torch.randn(x.shape, generator=gen).cuda()
+        layers.norm_backward(pl, x, dy, P, stats, dx, G, layers.norm_workspace(pl, 9, D, x.dtype, 0, D), gamma=0, beta=D)
+        assert bool(torch.isfinite(dx[0, good]).all()) and bool(torch.isfinite(G[0, D:2 * D]).all())
+        assert bool(torch.isnan(dx[0, [2, 4, 6]]).any(1).all())
+        pl.close()
+
+
+@pytest.mark.parametrize("D", [24, 600, 2500])
+def test_gradients_against_differences(D):
+    """Central differences of L = sum(dy * y) in 64 bits, along one direction of
+    every argument: off by O(h^2) of its third derivative (h = 2^-10 of inputs of
+    size one) and by the gradient's own bounds."""
+    import torch
+    from paper_2010_13359_amd import layers
+    pl, x, P, gen = _setup(1, 3, D, "f32", 0, D)
+    dy = torch.randn(x.shape, generator=gen).cuda()
+    y, dx, stats, G = torch.empty_like(x), torch.empty_like(x), torch.empty((1, 3, 2), device="cuda"), torch.zeros_like(P)
+    layers.norm_forward(pl, x, P, y, stats, gamma=0, beta=D)
+    layers.norm_backward(pl, x, dy, P, stats, dx, G, layers.norm_workspace(pl, 3, D, x.dtype, 0, D), gamma=0, beta=D)
+    ex, ep = torch.randn(x.shape, generator=gen).double(), torch.randn((2, D), generator=gen).double()
+    x64, p64, d64 = x.double().cpu(), P[0, :2 * D].double().cpu().view(2, D), dy.double().cpu()
+
+    def loss(s):
+        xs, ps = x64 + s * ex, p64 + s * ep
+        w = ref.norm_forward(xs[0], ps[0], ps[1], 1e-5)
+        return float((d64[0] * w[0]).sum())
+    h = 2.0 ** -10
+    slope = (loss(h) - loss(-h)) / (2 * h)
+    mine = float((dx.double().cpu() * ex).sum() + (G[0, :2 * D].double().cpu().view(2, D) * ep).sum())
+    size = float((dx.double().cpu() * ex).abs().sum() + (G[0, :2 * D].double().cpu().view(2, D) * ep).abs().sum())
+    assert abs(slope - mine) <= size * (h * h * 8 + (ref.depth(D) + 12) * ref.U)
+    pl.close()

@@ -1,0 +1,143 @@
+"""Host-side checks of the layer operators (no GPU needed): every function that
+include/dqgan_layers.h declares is exported and bound, and invalid calls are
+refused before the device is touched."""
+import ctypes
+import os
+import re
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2010_13359_amd import dqgan, layers
+    if not os.path.exists(dqgan.LIB_PATH):
+        from paper_2010_13359_amd import build
+        build.build()
+    return layers.load()
+
+
+def test_exports_every_declared_symbol(lib):
+    from paper_2010_13359_amd import layers
+    src = open(os.path.join(ROOT, "include", "dqgan_layers.h")).read()
+    names = sorted(set(re.findall(r"^dqgan_status\s*(dqgan_\w+)\s*\(", src, re.M)))
+    assert sorted(layers.EXPORTS) == names and len(names) == 10
+    for n in names:
+        assert hasattr(lib, n), n
+
+
+class FakePlan:
+    """Memory that begins with a plan's descriptor: all that the checks read
+    before they ask for the device.  Addresses are stand-ins."""
+
+    def __init__(self, d=5000, M=4, device=1 << 20):
+        from paper_2010_13359_amd import dqgan
+        self.desc = dqgan.Desc(d, (d + 1023) // 1024 * 1024, M, 1, None, dqgan.IDENTITY, 0, 0, 0, 0, 0)
+        self.memory = ctypes.create_string_buffer(4096)
+        ctypes.memmove(self.memory, ctypes.byref(self.desc), ctypes.sizeof(self.desc))
+        # a device number that is never the current one, wherever the plan keeps it: a call whose
+        # arguments are valid ends at that check
+        rest = ctypes.sizeof(self.desc)
+        ctypes.memset(ctypes.addressof(self.memory) + rest, 0x7F, 4096 - rest)
+
+    @property
+    def handle(self):
+        return ctypes.addressof(self.memory)
+
+
+OKP, ODD = 0x10000, 0x10008
+
+
+def _embed(**kw):
+    from paper_2010_13359_amd import layers
+    base = dict(offset=10, vocab=50, width=20, tokens=7, scale=1.0, type=1, index_type=1, reserved=0)
+    base.update(kw)
+    return layers.EmbedDesc(*base.values())
+
+
+def _norm(**kw):
+    from paper_2010_13359_amd import layers
+    base = dict(gamma=10, beta=100, width=64, tokens=7, eps=1e-5, type=1, reserved=0)
+    base.update(kw)
+    return layers.NormDesc(*base.values())
+
+
+def _distill(**kw):
+    from paper_2010_13359_amd import layers
+    base = dict(vocab=100, ld=104, tokens=7, k=5, temperature=1.0, type=1, reserved=0)
+    base.update(kw)
+    return layers.DistillDesc(*base.values())
+
+
+NAN, INF = float("nan"), float("inf")
+BAD_EMBED = [dict(vocab=0), dict(vocab=2 ** 31 - 1), dict(width=0), dict(width=2 ** 24 + 1), dict(offset=-1),
+             dict(offset=5000), dict(offset=4001), dict(vocab=250), dict(vocab=2 ** 31 - 2, width=2 ** 24), dict(tokens=-1),
+             dict(tokens=2 ** 30), dict(tokens=2 ** 31), dict(scale=NAN), dict(scale=INF), dict(type=3), dict(type=-1),
+             dict(index_type=2), dict(reserved=1)]
+BAD_NORM = [dict(gamma=-2), dict(gamma=4937), dict(beta=2 ** 40), dict(beta=73), dict(beta=10), dict(gamma=163), dict(width=0),
+            dict(width=5001), dict(width=2 ** 24 + 1, gamma=-1, beta=-1), dict(tokens=-1), dict(tokens=2 ** 30), dict(eps=-1e-9),
+            dict(eps=NAN), dict(eps=INF), dict(type=3), dict(reserved=1)]
+BAD_DISTILL = [dict(vocab=0), dict(vocab=105), dict(ld=2 ** 31), dict(tokens=-1), dict(tokens=2 ** 30), dict(k=0), dict(k=1025),
+               dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=NAN), dict(temperature=INF),
+               dict(temperature=2000.0), dict(type=3), dict(reserved=1)]
+
+
+@pytest.mark.parametrize("bad", BAD_EMBED)
+def test_embed_descriptors(lib, bad):
+    p, n = FakePlan(), ctypes.c_size_t()
+    d = ctypes.byref(_embed(**bad))
+    assert lib.dqgan_embed_bytes(p.handle, d, ctypes.byref(n)) == -1
+    assert lib.dqgan_embed_forward(p.handle, d, OKP, OKP, 5120, OKP, None) == -1
+    assert lib.dqgan_embed_backward(p.handle, d, OKP, OKP, OKP, 0, OKP, None) == -1
+
+
+@pytest.mark.parametrize("bad", BAD_NORM)
+def test_norm_descriptors(lib, bad):
+    p, n = FakePlan(), ctypes.c_size_t()
+    d = ctypes.byref(_norm(**bad))
+    assert lib.dqgan_norm_bytes(p.handle, d, ctypes.byref(n)) == -1
+    assert lib.dqgan_norm_forward(p.handle, d, OKP, OKP, 5120, OKP, OKP, None) == -1
+    assert lib.dqgan_norm_backward(p.handle, d, OKP, OKP, OKP, 5120, OKP, OKP, OKP, 0, OKP, None) == -1
+
+
+@pytest.mark.parametrize("bad", BAD_DISTILL)
+def test_distill_descriptors(lib, bad):
+    p, n = FakePlan(), ctypes.c_size_t()
+    d = ctypes.byref(_distill(**bad))
+    assert lib.dqgan_distill_bytes(p.handle, d, ctypes.byref(n)) == -1
+    assert lib.dqgan_distill_forward(p.handle, d, OKP, OKP, OKP, OKP, OKP, OKP, OKP, None) == -1
+    assert lib.dqgan_distill_backward(p.handle, d, OKP, OKP, OKP, OKP, OKP, OKP, None) == -1
+    assert lib.dqgan_distill_fused(p.handle, d, OKP, OKP, OKP, OKP, OKP, OKP, OKP, None) == -1
+
+
+def test_pointers(lib):
+    """Each required pointer missing or misaligned, each optional one
+    misaligned.  The valid call itself ends at the device check."""
+    p = FakePlan()
+    e, n, k = (ctypes.byref(x) for x in (_embed(), _norm(), _distill()))
+    # function, arguments, positions of required and of optional pointers
+    calls = [(lib.dqgan_embed_forward, [e, OKP, OKP, 5120, OKP], [1, 2, 4], []),
+             (lib.dqgan_embed_backward, [e, OKP, OKP, OKP, 0, OKP], [1, 2, 3, 5], []),
+             (lib.dqgan_norm_forward, [n, OKP, OKP, 5120, OKP, OKP], [1, 2, 4], [5]),
+             (lib.dqgan_norm_backward, [n, OKP, OKP, OKP, 5120, OKP, OKP, OKP, 0, OKP], [1, 2, 3, 5, 7, 9], [6]),
+             (lib.dqgan_distill_forward, [k, OKP, OKP, OKP, OKP, OKP, OKP, OKP], [1, 2, 3, 5, 6], [4, 7]),
+             (lib.dqgan_distill_backward, [k, OKP, OKP, OKP, OKP, OKP, OKP], [1, 2, 3, 5, 6], [4]),
+             (lib.dqgan_distill_fused, [k, OKP, OKP, OKP, OKP, OKP, OKP, OKP], [1, 2, 3, 5, 6], [4, 7])]
+    for f, args, required, optional in calls:
+        assert f(p.handle, *args, None) in (-1, -4)          # another device, or none here
+        assert f(None, *args, None) == -1
+        assert f(p.handle, None, *args[1:], None) == -1
+        for at in required + optional:
+            odd = args[:at] + [ODD] + args[at + 1:]
+            assert f(p.handle, *odd, None) == -2, (f.__name__, at)
+        for at in required:
+            gone = args[:at] + [None] + args[at + 1:]
+            assert f(p.handle, *gone, None) == -1, (f.__name__, at)
+    for f, d in ((lib.dqgan_embed_bytes, e), (lib.dqgan_norm_bytes, n), (lib.dqgan_distill_bytes, k)):
+        assert f(p.handle, d, None) == -1
+        assert f(None, d, ctypes.byref(ctypes.c_size_t())) == -1
+    # the parameters' row stride: the plan's or 0
+    assert lib.dqgan_embed_forward(p.handle, e, OKP, OKP, 5000, OKP, None) == -1
+    assert lib.dqgan_norm_forward(p.handle, n, OKP, OKP, 1024, OKP, OKP, None) == -1
