@@ -49,11 +49,13 @@ struct Message {
     float slots[4][16];
 };
 
-// Reads a message and the student's logits at its entries, and makes t and
-// log t.  Every thread of the workgroup calls it.  Returns 0 if no entry counts,
-// 1 if their indices ascend (so that none comes twice), else 2.
+// Reads a message and the student's logits at its entries (those that lie in
+// columns [begin, end), or all of them from `gathered`), and makes t and log t.
+// Every thread of the workgroup calls it.  Returns 0 if no entry counts, 1 if
+// their indices ascend (so that none comes twice), else 2.
 template <typename T, int W>
-__device__ int teacher(const DistillArgs &a, int64_t row, const T *z, Message &s) {
+__device__ int teacher(const DistillArgs &a, int64_t row, const T *z, const float *gathered, int64_t begin, int64_t end,
+                       Message &s) {
     const float *val = a.val + row * a.k;
     const uint32_t *from = a.idx + row * a.k;
     float top = kNone;
@@ -68,7 +70,10 @@ __device__ int teacher(const DistillArgs &a, int64_t row, const T *z, Message &s
         if (!counts) continue;
         have |= 1;
         top = fmaxf(top, v);
-        s.z[j] = static_cast<float>(z[i]);
+        if (gathered)
+            s.z[j] = gathered[j];
+        else if (i >= begin && i < end)
+            s.z[j] = static_cast<float>(z[i]);
     }
     have = (__syncthreads_or(have & 1) ? 1 : 0) | (__syncthreads_or(have & 2) ? 2 : 0);
     top = group_max<W>(top, s.slots[0]);
@@ -125,58 +130,106 @@ __device__ __forceinline__ void forget(V &raw) {
     raw = __builtin_bit_cast(V, w);
 }
 
+// NV vectors of 16 bytes per lane of a row's columns [0, V), and the last V % kPer
+// columns one each in the first lanes.  Vectors beyond the row are -inf.
+template <typename T, int W, int NV, bool STREAM>
+struct Logits {
+    typedef typename Vec16<T>::type Raw;
+    typedef typename Vec16<T>::packed Packed;
+    typedef typename Vec16<T>::wide Wide;
+    static constexpr int kPer = Vec16<T>::kPer;
+    static constexpr bool FINE = sizeof(T) == 4;
+    Raw raw[NV];
+    float last;
+
+    __device__ __forceinline__ void load(const T *from, int vectors, int rest) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int q = threadIdx.x + 64 * W * v;
+            if (q < vectors) {
+                const Packed *p = reinterpret_cast<const Packed *>(from) + q;
+                raw[v] = STREAM ? __builtin_nontemporal_load(p) : *p;
+            } else {
+                raw[v] = static_cast<T>(kNone);
+            }
+        }
+        last = static_cast<int>(threadIdx.x) < rest ? static_cast<float>(from[kPer * vectors + threadIdx.x]) : kNone;
+    }
+    __device__ __forceinline__ float largest() const {
+        float top = last;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const Wide f = __builtin_convertvector(raw[v], Wide);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) top = fmaxf(top, f[i]);
+        }
+        return top;
+    }
+    __device__ __forceinline__ float sum(const DistillArgs &a, float ref) {
+        float sum = exp_of<FINE>(a, last, ref);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            forget(raw[v]);
+            const Wide f = __builtin_convertvector(raw[v], Wide);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) sum += exp_of<FINE>(a, f[i], ref);
+        }
+        return sum;
+    }
+    // s * over
+    __device__ __forceinline__ void gradient(const DistillArgs &a, float largest, float over, T *to, int vectors, int rest) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int q = threadIdx.x + 64 * W * v;
+            forget(raw[v]);
+            Wide f = __builtin_convertvector(raw[v], Wide);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) f[i] = exp_of<FINE>(a, f[i], largest) * over;
+            if (q < vectors) {
+                Packed *p = reinterpret_cast<Packed *>(to) + q;
+                const Raw r = __builtin_convertvector(f, Raw);
+                if (STREAM)
+                    __builtin_nontemporal_store(r, p);
+                else
+                    *p = r;
+            }
+        }
+        if (static_cast<int>(threadIdx.x) < rest)
+            to[kPer * vectors + threadIdx.x] = static_cast<T>(exp_of<FINE>(a, last, largest) * over);
+    }
+};
+
+// Zeros of columns [begin, end) of a row.
+template <typename T, int W>
+__device__ void clear(T *to, int64_t begin, int64_t end) {
+    for (int64_t c = begin + 8 * threadIdx.x; c < end; c += 8 * 64 * W) store8(to + c, end - c, f32x8(0.0f));
+}
+
 // One workgroup per token, whose logits stay in registers between the
-// statistics and the gradient: NV vectors of eight per lane, and the last
-// V % 8 one each in the first lanes.  LOSS: the statistics and the loss; GRAD:
-// dz, from the statistics just made or (LOSS not) from `stats`.
-template <typename T, int W, int NV, bool LOSS, bool GRAD>
+// statistics and the gradient.  LOSS: the statistics and the loss; GRAD: dz,
+// from the statistics just made or (LOSS not) from `stats`.
+template <typename T, int W, int NV, bool LOSS, bool GRAD, bool STREAM>
 __global__ __launch_bounds__(64 * W) void k_distill_row(const T *z, DistillArgs a, float *loss, float *stats, T *dz) {
     constexpr bool FINE = sizeof(T) == 4;
-    typedef typename Vec8<T>::type Raw;
-    typedef typename Vec8<T>::packed Packed;
+    constexpr int kPer = Vec16<T>::kPer;
     __shared__ Message s;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x;
     const T *from = z + row * a.ld;
     T *to = dz + row * a.ld;
     const float weight = a.weight ? a.weight[row] : 1.0f;
-    const int vectors = static_cast<int>(a.V >> 3), rest = static_cast<int>(a.V & 7);
+    const int vectors = static_cast<int>(a.V / kPer), rest = static_cast<int>(a.V % kPer);
     int have = 0;
     Softmax x{0.0f, 0.0f};
-    Raw raw[NV];
-    float last = kNone;
+    Logits<T, W, NV, STREAM> l;
     if (weight != 0.0f) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int q = tid + 64 * W * v;
-            if (q < vectors)
-                raw[v] = reinterpret_cast<const Packed *>(from)[q];
-            else
-                raw[v] = static_cast<T>(kNone);
-        }
-        if (tid < rest) last = static_cast<float>(from[8 * vectors + tid]);
-        have = teacher<T, W>(a, row, from, s);
+        l.load(from, vectors, rest);
+        have = teacher<T, W>(a, row, from, nullptr, 0, a.V, s);
     }
     if (have != 0) {
         if (LOSS) {
-            float top = last;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const f32x8 f = __builtin_convertvector(raw[v], f32x8);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, f[i]);
-            }
-            x.largest = group_max<W>(top, s.slots[2]);
-            const float ref = reference(x.largest);
-            float sum = exp_of<FINE>(a, last, ref);
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                forget(raw[v]);
-                const f32x8 f = __builtin_convertvector(raw[v], f32x8);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum += exp_of<FINE>(a, f[i], ref);
-            }
-            x.total = group_sum<W>(sum, s.slots[3]);
+            x.largest = group_max<W>(l.largest(), s.slots[2]);
+            x.total = group_sum<W>(l.sum(a, reference(x.largest)), s.slots[3]);
             if (x.largest == kNone && x.total == 0.0f) have = 0;
         } else {
             x.largest = stats[2 * row];
@@ -197,58 +250,73 @@ __global__ __launch_bounds__(64 * W) void k_distill_row(const T *z, DistillArgs 
     }
     if (GRAD) {
         if (have == 0) {
-            for (int64_t c = 8 * tid; c < a.ld; c += 8 * 64 * W) store8(to + c, a.ld - c, f32x8(0.0f));
+            clear<T, W>(to, 0, a.ld);
             return;
         }
         const float coef = weight * a.T, over = coef / x.total;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int q = tid + 64 * W * v;
-            forget(raw[v]);
-            f32x8 f = __builtin_convertvector(raw[v], f32x8);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = exp_of<FINE>(a, f[i], x.largest) * over;
-            if (q < vectors) reinterpret_cast<Packed *>(to)[q] = __builtin_convertvector(f, Raw);
-        }
-        if (tid < rest) to[8 * vectors + tid] = static_cast<T>(exp_of<FINE>(a, last, x.largest) * over);
-        for (int64_t c = a.V + tid; c < a.ld; c += 64 * W) to[c] = static_cast<T>(0.0f);
+        l.gradient(a, x.largest, over, to, vectors, rest);
+        clear<T, W>(to, a.V, a.ld);
         __syncthreads();
         for (int j = tid; j < a.k; j += 64 * W)
             if (s.idx[j] != UINT32_MAX) to[s.idx[j]] = static_cast<T>(entry_gradient<FINE>(a, s, have, x, coef, j));
     }
 }
 
-// Rows that do not fit the registers: read twice.
+// Few tokens: a row's columns are shared out in slices of kSlice bytes.
+constexpr int kSliceVectors = 4;
+template <typename T>
+constexpr int kSlice = 64 * 4 * kSliceVectors * Vec16<T>::kPer;
+
+// Statistics of one slice, and the student's logits at the message's entries
+// (before dz, which may be z, is written).
+template <typename T>
+__global__ __launch_bounds__(256) void k_distill_part(const T *z, DistillArgs a, Softmax *part, float *gathered) {
+    __shared__ float slots[2][4];
+    const int64_t row = blockIdx.y, begin = static_cast<int64_t>(blockIdx.x) * kSlice<T>;
+    if (a.weight && a.weight[row] == 0.0f) return;
+    const int64_t n = a.V - begin < kSlice<T> ? a.V - begin : kSlice<T>;
+    const T *from = z + row * a.ld;
+    Logits<T, 4, kSliceVectors, false> l;
+    l.load(from + begin, static_cast<int>(n / Vec16<T>::kPer), static_cast<int>(n % Vec16<T>::kPer));
+    for (int64_t j = blockIdx.x * 256 + threadIdx.x; j < a.k; j += 256 * gridDim.x) {
+        const uint32_t i = a.idx[row * a.k + j];
+        if (i < a.V) gathered[row * a.k + j] = static_cast<float>(from[i]);
+    }
+    const float largest = group_max<4>(l.largest(), slots[0]);
+    const float total = group_sum<4>(l.sum(a, reference(largest)), slots[1]);
+    if (threadIdx.x == 0) part[row * gridDim.x + blockIdx.x] = Softmax{largest, total};
+}
+
+// LOSS: joins the slices' statistics; the first slice's workgroup writes them
+// and the loss.  GRAD: dz of one slice.
 template <typename T, bool LOSS, bool GRAD>
-__global__ __launch_bounds__(1024) void k_distill_long(const T *z, DistillArgs a, float *loss, float *stats, T *dz) {
+__global__ __launch_bounds__(256) void k_distill_slice(const T *z, DistillArgs a, int slices, const Softmax *part,
+                                                       const float *gathered, float *loss, float *stats, T *dz) {
     constexpr bool FINE = sizeof(T) == 4;
-    constexpr int W = 16;
     __shared__ Message s;
-    const int64_t row = blockIdx.x;
+    const int64_t row = blockIdx.y, begin = static_cast<int64_t>(blockIdx.x) * kSlice<T>;
+    const int64_t n = a.V - begin < kSlice<T> ? a.V - begin : kSlice<T>;
+    const int vectors = static_cast<int>(n / Vec16<T>::kPer), rest = static_cast<int>(n % Vec16<T>::kPer);
+    const int tid = threadIdx.x;
     const T *from = z + row * a.ld;
     T *to = dz + row * a.ld;
     const float weight = a.weight ? a.weight[row] : 1.0f;
     int have = 0;
-    Softmax x{kNone, 0.0f};
-    if (weight != 0.0f) have = teacher<T, W>(a, row, from, s);
+    Softmax x{0.0f, 0.0f};
+    Logits<T, 4, kSliceVectors, false> l;
+    if (weight != 0.0f) {
+        if (GRAD) l.load(from + begin, vectors, rest);
+        have = teacher<T, 4>(a, row, from, LOSS ? gathered + row * a.k : nullptr, begin, begin + n, s);
+    }
     if (have != 0) {
         if (LOSS) {
-            for (int64_t c = 8 * threadIdx.x; c < a.V; c += 8 * 64 * W) {
-                const f32x8 f = load8(from + c, a.V - c, kNone);
-                float top = x.largest;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, f[i]);
-                if (top > x.largest) {
-                    x.total *= exp_of<FINE>(a, x.largest, top);
-                    x.largest = top;
-                }
-                const float ref = reference(x.largest);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x.total += exp_of<FINE>(a, f[i], ref);
-            }
-            const float mine = x.largest;
-            x.largest = group_max<W>(mine, s.slots[2]);
-            x.total = group_sum<W>(x.total * exp_of<FINE>(a, mine, reference(x.largest)), s.slots[3]);
+            const Softmax *p = part + row * slices;
+            float top = kNone, sum = 0.0f;
+            for (int i = tid; i < slices; i += 256) top = fmaxf(top, p[i].largest);
+            x.largest = group_max<4>(top, s.slots[2]);
+            for (int i = tid; i < slices; i += 256)
+                sum += p[i].total * exp_of<FINE>(a, p[i].largest, reference(x.largest));
+            x.total = group_sum<4>(sum, s.slots[3]);
             if (x.largest == kNone && x.total == 0.0f) have = 0;
         } else {
             x.largest = stats[2 * row];
@@ -256,10 +324,10 @@ __global__ __launch_bounds__(1024) void k_distill_long(const T *z, DistillArgs a
             if (x.total == 0.0f) have = 0;
         }
     }
-    if (LOSS) {
+    if (LOSS && blockIdx.x == 0) {
         float value = 0.0f;
-        if (have != 0) value = weight * a.T * a.T * loss_of<W>(a, s, x, s.slots[0]);
-        if (threadIdx.x == 0) {
+        if (have != 0) value = weight * a.T * a.T * loss_of<4>(a, s, x, s.slots[0]);
+        if (tid == 0) {
             loss[row] = value;
             if (stats) {
                 stats[2 * row] = have ? x.largest : 0.0f;
@@ -268,43 +336,59 @@ __global__ __launch_bounds__(1024) void k_distill_long(const T *z, DistillArgs a
         }
     }
     if (GRAD) {
-        const float coef = weight * a.T, over = coef / x.total;
-        for (int64_t c = 8 * threadIdx.x; c < a.ld; c += 8 * 64 * W) {
-            f32x8 f = 0.0f;
-            if (have != 0) {
-                f = load8(from + c, a.V - c, kNone);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = c + i < a.V ? exp_of<FINE>(a, f[i], x.largest) * over : 0.0f;
-            }
-            store8(to + c, a.ld - c, f);
+        if (begin + n == a.V) clear<T, 4>(to, a.V, a.ld);
+        if (have == 0) {
+            clear<T, 4>(to, begin, begin + n);
+            return;
         }
-        if (have == 0) return;
+        const float coef = weight * a.T, over = coef / x.total;
+        l.gradient(a, x.largest, over, to + begin, vectors, rest);
         __syncthreads();
-        for (int j = threadIdx.x; j < a.k; j += 64 * W)
-            if (s.idx[j] != UINT32_MAX) to[s.idx[j]] = static_cast<T>(entry_gradient<FINE>(a, s, have, x, coef, j));
+        for (int j = tid; j < a.k; j += 256) {
+            const uint32_t i = s.idx[j];
+            if (i != UINT32_MAX && i >= begin && i < begin + n)
+                to[i] = static_cast<T>(entry_gradient<FINE>(a, s, have, x, coef, j));
+        }
     }
 }
 
-// f(W, NV) with the smallest row shape that holds V, or (0, 0).  A lane keeps
-// up to 64 registers of logits.
-template <typename T, typename F>
-void with_shape(int64_t V, F &&f) {
+// f(W, NV) with the smallest row shape that holds `bytes` (up to kRowMost).  A lane
+// keeps up to 64 registers of logits.
+template <typename F>
+void with_shape(int64_t bytes, F &&f) {
     using std::integral_constant;
-    constexpr int MOST = sizeof(T) == 4 ? 8 : 16;
-    if (V <= 2048)
+    if (bytes <= 4096)
         f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    else if (V <= 4096)
+    else if (bytes <= 8192)
         f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-    else if (V <= 8192)
+    else if (bytes <= 16384)
         f(integral_constant<int, 4>{}, integral_constant<int, 4>{});
-    else if (V <= 512 * 4 * MOST)
-        f(integral_constant<int, 4>{}, integral_constant<int, MOST>{});
-    else if (V <= 512 * 8 * MOST)
-        f(integral_constant<int, 8>{}, integral_constant<int, MOST>{});
-    else if (V <= 512 * 16 * MOST)
-        f(integral_constant<int, 16>{}, integral_constant<int, MOST>{});
+    else if (bytes <= 32768)
+        f(integral_constant<int, 4>{}, integral_constant<int, 8>{});
+    else if (bytes <= 65536)
+        f(integral_constant<int, 4>{}, integral_constant<int, 16>{});
+    else if (bytes <= 131072)
+        f(integral_constant<int, 8>{}, integral_constant<int, 16>{});
     else
-        f(integral_constant<int, 0>{}, integral_constant<int, 0>{});
+        f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+}
+
+// Rows are shared out in slices where a row does not fit a workgroup's
+// registers, and where it takes a CU's whole and there are so few that most CUs
+// would have none: loss and gradient of 64 rows of 128000 bf16 logits 15.3 us in
+// slices and 21.3 by rows, of 256 rows 43 and 35.
+constexpr int64_t kRowMost = 262144, kRowFewer = 131072, kFewRows = 96;
+bool split(int64_t rows, int64_t bytes) { return bytes > kRowMost || (bytes > kRowFewer && rows <= kFewRows); }
+int64_t slices_of(int64_t bytes) { return ceil_div(bytes, 64 * 4 * kSliceVectors * 16); }
+
+// Whether long rows (16 vectors a lane) pass by the caches: loss and gradient of
+// 32000 bf16 logits, read and written, of 33 MB in all 11.5 us so and 11.9
+// with ordinary accesses, of 132 MB 28.6 / 33.1, 526 MB 102 / 115; of 128000
+// logits 8 MB 20.7 / 18.8, 1050 MB 221 / 236, 2500 MB 580 / 563.
+constexpr double kStreamFrom = 64e6, kStreamUpTo = 1.4e9;
+bool streams(int64_t rows, int64_t bytes) {
+    const double total = 2.0 * static_cast<double>(rows) * static_cast<double>(bytes);
+    return total >= kStreamFrom && total <= kStreamUpTo;
 }
 
 dqgan_status check(dqgan_plan P, const dqgan_distill_desc *d) {
@@ -324,31 +408,61 @@ dqgan_status check_inputs(const dqgan_distill_desc *d, const void *z, const floa
     return check_ptr(weight, false);
 }
 
+size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
+
+// Slices' statistics, then the student's logits at the entries.
+size_t part_bytes(int64_t rows, int64_t row_bytes) {
+    return round256(sizeof(Softmax) * static_cast<size_t>(rows * slices_of(row_bytes)));
+}
+int64_t row_bytes_of(const dqgan_distill_desc *d) { return d->vocab * (d->type == DQGAN_F32 ? 4 : 2); }
+
+DistillArgs from_row(DistillArgs a, int64_t r) {
+    a.val += r * a.k;
+    a.idx += r * a.k;
+    if (a.weight) a.weight += r;
+    return a;
+}
+
 template <bool LOSS, bool GRAD>
 dqgan_status run(dqgan_plan P, const dqgan_distill_desc *d, const void *z, const float *val, const uint32_t *idx,
-                 const float *weight, float *loss, float *stats, void *dz, hipStream_t st) {
+                 const float *weight, float *loss, float *stats, void *dz, void *workspace, hipStream_t st) {
     const DistillArgs a{val, idx, weight, d->vocab, d->ld, d->k, d->temperature, 1.0f / d->temperature,
                         static_cast<float>(1.4426950408889634 / d->temperature)};
-    const int64_t rows = d->tokens * P->desc.M;
+    const int64_t rows = d->tokens * P->desc.M, bytes = row_bytes_of(d);
+    if (split(rows, bytes)) {
+        const uint32_t slices = static_cast<uint32_t>(slices_of(bytes));
+        Softmax *part = static_cast<Softmax *>(workspace);
+        float *gathered = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(rows, bytes));
+        for (int64_t r = 0; r < rows; r += 65535) {  // a launch's most in the second dimension
+            const uint32_t n = static_cast<uint32_t>(rows - r < 65535 ? rows - r : 65535);
+            const DistillArgs b = from_row(a, r);
+            with_type(d->type, [&](auto t) {
+                using T = decltype(t);
+                const T *from = static_cast<const T *>(z) + r * a.ld;
+                if (LOSS) k_distill_part<T><<<dim3(slices, n), 256, 0, st>>>(from, b, part + r * slices, gathered + r * a.k);
+                k_distill_slice<T, LOSS, GRAD><<<dim3(GRAD ? slices : 1, n), 256, 0, st>>>(
+                    from, b, static_cast<int>(slices), part + r * slices, gathered + r * a.k, LOSS ? loss + r : nullptr,
+                    stats ? stats + 2 * r : stats, static_cast<T *>(dz) + (GRAD ? r * a.ld : 0));
+            });
+        }
+        return launched();
+    }
     // a launch has fewer than 2^32 threads
-    constexpr int64_t kMost = int64_t(1) << 22;
+    constexpr int64_t kMost = int64_t(1) << 21;
     for (int64_t r = 0; r < rows; r += kMost) {
         const uint32_t n = static_cast<uint32_t>(rows - r < kMost ? rows - r : kMost);
-        DistillArgs b = a;
-        b.val += r * a.k;
-        b.idx += r * a.k;
-        if (b.weight) b.weight += r;
+        const DistillArgs b = from_row(a, r);
         with_type(d->type, [&](auto t) {
             using T = decltype(t);
             const T *from = static_cast<const T *>(z) + r * a.ld;
             T *to = static_cast<T *>(dz) + (GRAD ? r * a.ld : 0);
             float *l = loss ? loss + r : loss, *x = stats ? stats + 2 * r : stats;
-            with_shape<T>(a.V, [&](auto w, auto nv) {
+            with_shape(bytes, [&](auto w, auto nv) {
                 constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-                if constexpr (W == 0)
-                    k_distill_long<T, LOSS, GRAD><<<n, 1024, 0, st>>>(from, b, l, x, to);
+                if (GRAD && NV == 16 && streams(rows, bytes))
+                    k_distill_row<T, W, NV, LOSS, GRAD, GRAD && NV == 16><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
                 else
-                    k_distill_row<T, W, NV, LOSS, GRAD><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
+                    k_distill_row<T, W, NV, LOSS, GRAD, false><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
             });
         });
     }
@@ -370,10 +484,11 @@ dqgan_status dqgan_distill_forward(dqgan_plan P, const dqgan_distill_desc *d, co
     DQ_TRY(check_inputs(d, z, val, idx, weight));
     DQ_TRY(check_ptr(loss, any));
     DQ_TRY(check_ptr(stats, any));
-    DQ_TRY(check_ptr(workspace, false));
+    DQ_TRY(check_ptr(workspace, any && split(d->tokens * P->desc.M, row_bytes_of(d))));
     DQ_TRY(check_device(P));
     if (!any) return DQGAN_OK;
-    return run<true, false>(P, d, z, val, idx, weight, loss, stats, nullptr, static_cast<hipStream_t>(stream));
+    return run<true, false>(P, d, z, val, idx, weight, loss, stats, nullptr, workspace,
+                            static_cast<hipStream_t>(stream));
 }
 
 dqgan_status dqgan_distill_backward(dqgan_plan P, const dqgan_distill_desc *d, const void *z, const float *val,
@@ -386,7 +501,7 @@ dqgan_status dqgan_distill_backward(dqgan_plan P, const dqgan_distill_desc *d, c
     DQ_TRY(check_ptr(dz, any));
     DQ_TRY(check_device(P));
     if (!any) return DQGAN_OK;
-    return run<false, true>(P, d, z, val, idx, weight, nullptr, const_cast<float *>(stats), dz,
+    return run<false, true>(P, d, z, val, idx, weight, nullptr, const_cast<float *>(stats), dz, nullptr,
                             static_cast<hipStream_t>(stream));
 }
 
@@ -398,16 +513,18 @@ dqgan_status dqgan_distill_fused(dqgan_plan P, const dqgan_distill_desc *d, cons
     DQ_TRY(check_inputs(d, z, val, idx, weight));
     DQ_TRY(check_ptr(loss, any));
     DQ_TRY(check_ptr(dz, any));
-    DQ_TRY(check_ptr(workspace, false));
+    DQ_TRY(check_ptr(workspace, any && split(d->tokens * P->desc.M, row_bytes_of(d))));
     DQ_TRY(check_device(P));
     if (!any) return DQGAN_OK;
-    return run<true, true>(P, d, z, val, idx, weight, loss, nullptr, dz, static_cast<hipStream_t>(stream));
+    return run<true, true>(P, d, z, val, idx, weight, loss, nullptr, dz, workspace,
+                           static_cast<hipStream_t>(stream));
 }
 
 dqgan_status dqgan_distill_bytes(dqgan_plan P, const dqgan_distill_desc *d, size_t *bytes) {
     DQ_TRY(check(P, d));
     if (!bytes) return DQGAN_EINVAL;
-    *bytes = 0;
+    const int64_t rows = d->tokens * P->desc.M, row = row_bytes_of(d);
+    *bytes = rows > 0 && split(rows, row) ? part_bytes(rows, row) + sizeof(float) * static_cast<size_t>(rows * d->k) : 0;
     return DQGAN_OK;
 }
 

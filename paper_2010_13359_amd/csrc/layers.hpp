@@ -69,6 +69,15 @@ struct Vec8 {
     typedef T packed __attribute__((ext_vector_type(8), aligned(sizeof(T))));
 };
 
+// Sixteen bytes of a row: kPer elements.
+template <typename T>
+struct Vec16 {
+    static constexpr int kPer = 16 / sizeof(T);
+    typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
+    typedef T packed __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+    typedef float wide __attribute__((ext_vector_type(16 / sizeof(T))));
+};
+
 // p[0..8), of which n are there; the others come as `fill`.
 template <typename T>
 __device__ __forceinline__ f32x8 load8(const T *p, int64_t n, float fill = 0.0f) {
@@ -122,7 +131,26 @@ __device__ __forceinline__ float wave_max(float x) {
     return lane63(x);
 }
 
-// Sum over the W waves of a workgroup, in every lane.  `slot` is W floats of
+// Sum and maximum over groups of W consecutive lanes (4, 8 or 16), in each.
+template <int W>
+__device__ __forceinline__ float lanes_sum(float x) {
+    x += dpp_or<0xB1, 0xF>(0.0f, x);
+    x += dpp_or<0x4E, 0xF>(0.0f, x);
+    if (W > 4) x += dpp_or<0x141, 0xF>(0.0f, x);
+    if (W > 8) x += dpp_or<0x140, 0xF>(0.0f, x);
+    return x;
+}
+template <int W>
+__device__ __forceinline__ float lanes_max(float x) {
+    x = fmaxf(x, dpp_or<0xB1, 0xF>(x, x));
+    x = fmaxf(x, dpp_or<0x4E, 0xF>(x, x));
+    if (W > 4) x = fmaxf(x, dpp_or<0x141, 0xF>(x, x));
+    if (W > 8) x = fmaxf(x, dpp_or<0x140, 0xF>(x, x));
+    return x;
+}
+
+// Sum over the W waves of a workgroup, in every lane: each wave reads the W
+// sums side by side in its lanes and adds them up again.  `slot` is W floats of
 // LDS that the next call does not use again (two slots in turn).
 template <int W>
 __device__ __forceinline__ float group_sum(float x, float *slot) {
@@ -130,10 +158,7 @@ __device__ __forceinline__ float group_sum(float x, float *slot) {
     if (W == 1) return x;
     if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = x;
     __syncthreads();
-    float s = slot[0];
-#pragma unroll
-    for (int w = 1; w < W; ++w) s += slot[w];
-    return s;
+    return lanes_sum<W>(slot[threadIdx.x & (W - 1)]);
 }
 template <int W>
 __device__ __forceinline__ float group_max(float x, float *slot) {
@@ -141,10 +166,7 @@ __device__ __forceinline__ float group_max(float x, float *slot) {
     if (W == 1) return x;
     if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = x;
     __syncthreads();
-    float s = slot[0];
-#pragma unroll
-    for (int w = 1; w < W; ++w) s = fmaxf(s, slot[w]);
-    return s;
+    return lanes_max<W>(slot[threadIdx.x & (W - 1)]);
 }
 
 }  // namespace dq

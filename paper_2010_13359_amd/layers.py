@@ -13,7 +13,7 @@ import ctypes
 import torch
 
 from . import dqgan
-from .dqgan import F32, U32, _check, _ptr, _stream
+from .dqgan import F32, U32, _check, _ptr
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 INDEX_TYPES = {torch.int32: 0, torch.int64: 1}
@@ -69,27 +69,47 @@ def load():
 
 
 def _type(dtype, name):
-    if dtype not in TYPES:
+    t = TYPES.get(dtype)
+    if t is None:
         raise TypeError("%s: dtype %s, expected one of %s" % (name, dtype, ", ".join(str(t) for t in TYPES)))
-    return TYPES[dtype]
+    return t
 
 
-def _rows(plan, t, name, width=None):
-    """[M][tokens] or [M][tokens][width] of a tensor that says how many tokens a call has."""
-    dims = 2 if width is None else 3
+# descriptors by their values and the plan's sizes, with the workspace that the
+# library asks for: neither depends on anything else
+_descs = {}
+
+
+def _desc(plan, cls, fn, *fields):
+    """(reference to the descriptor, bytes of workspace)."""
+    key = (cls, plan.M, plan.d, plan.ld, fields)
+    hit = _descs.get(key)
+    if hit is None:
+        d, n = cls(*fields), ctypes.c_size_t()
+        _check(fn, getattr(load(), fn)(plan.handle, ctypes.byref(d), ctypes.byref(n)))
+        if len(_descs) >= 4096:
+            _descs.clear()
+        hit = _descs[key] = (ctypes.byref(d), n.value)
+    return hit
+
+
+def _shape(plan, t, name, dims):
+    """Shape of the tensor that says what sizes a call has."""
     if not isinstance(t, torch.Tensor) or t.dim() != dims or t.shape[0] != plan.M:
-        raise ValueError("%s: expected a tensor of [%d][tokens]%s" % (name, plan.M, "" if width is None else "[width]"))
-    return t.shape[1]
+        raise ValueError("%s: expected a tensor of [%d][tokens]%s" % (name, plan.M, "[width]" if dims == 3 else ""))
+    return t.shape
 
 
 def _like(plan, t, name, shape, dtypes):
-    """Device pointer of a tensor that has to have this shape."""
+    """Device pointer of a tensor that has to have this shape (None: NULL)."""
     if t is None:
         return None
-    p = _ptr(t, name, 0, dtypes, plan.device)
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    return p or None
+    # the usual case by the fewest attribute reads; what fails here is named below
+    if (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype in dtypes and t.get_device() == plan.device
+            and t.is_contiguous()):
+        return t.data_ptr() or None
+    _ptr(t, name, 0, dtypes, plan.device)
+    raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
 
 
 def _params(plan, P):
@@ -104,15 +124,17 @@ def _params(plan, P):
 
 def _workspace(plan, t, need):
     """Pointer of the caller's workspace: any contiguous tensor of enough bytes."""
-    if t is None and need:
-        raise ValueError("workspace: the call needs %d bytes" % need)
+    if t is None:
+        if need:
+            raise ValueError("workspace: the call needs %d bytes" % need)
+        return None
     return _ptr(t, "workspace", need, None, plan.device) or None
 
 
-def _bytes(fn, plan, desc):
-    n = ctypes.c_size_t()
-    _check(fn, getattr(load(), fn)(plan.handle, ctypes.byref(desc), ctypes.byref(n)))
-    return n.value
+def _on(plan, stream):
+    if stream is None:  # the plan's device is the current one, or the library refuses the call
+        return torch._C._cuda_getCurrentRawStream(plan.device)
+    return stream.cuda_stream
 
 
 def _new(plan, n):
@@ -123,49 +145,50 @@ def _new(plan, n):
 # embedding
 
 
+def _embed(plan, tokens, x, name, vocab, offset, scale):
+    """Descriptor, workspace and token pointer of a call whose activations are x."""
+    shape = _shape(plan, x, name, 3)
+    tok = _like(plan, tokens, "tokens", shape[:2], INDEX_TYPES)
+    return _desc(plan, EmbedDesc, "dqgan_embed_bytes", offset, vocab, shape[2], shape[1], scale, _type(x.dtype, name),
+                 INDEX_TYPES.get(getattr(tokens, "dtype", None), 0), 0) + (tok,)
+
+
 def embed_forward(plan, tokens, P, out, vocab, offset=0, scale=1.0, stream=None):
     """out[m][n] = scale * row tokens[m][n] of worker m's table, which lies at
     `offset` of its row of P ([vocab][width]); 0 where the token is below 0 or
     at or beyond vocab.  tokens int32 or int64 [M][tokens]; P [M][ld], or [ld]
     for all workers; out [M][tokens][width]."""
-    n = _rows(plan, out, "out", True)
-    d = EmbedDesc(offset, vocab, out.shape[2], n, scale, _type(out.dtype, "out"), 0, 0)
-    tok = _like(plan, tokens, "tokens", (plan.M, n), tuple(INDEX_TYPES))
-    d.index_type = INDEX_TYPES.get(getattr(tokens, "dtype", None), 0)
+    d, _, tok = _embed(plan, tokens, out, "out", vocab, offset, scale)
     p, ldp = _params(plan, P)
-    _check("dqgan_embed_forward", load().dqgan_embed_forward(plan.handle, ctypes.byref(d), tok, p, ldp,
-                                                             _like(plan, out, "out", out.shape, tuple(TYPES)),
-                                                             _stream(stream)))
+    _check("dqgan_embed_forward", load().dqgan_embed_forward(plan.handle, d, tok, p, ldp,
+                                                             _like(plan, out, "out", out.shape, TYPES),
+                                                             _on(plan, stream)))
 
 
 def embed_workspace(plan, tokens, vocab, width, dtype, index_dtype=torch.int64, offset=0):
-    """A workspace for embed_backward with up to `tokens` tokens per worker."""
-    d = EmbedDesc(offset, vocab, width, tokens, 1.0, _type(dtype, "dtype"), INDEX_TYPES[index_dtype], 0)
-    return _new(plan, _bytes("dqgan_embed_bytes", plan, d))
+    """A workspace for embed_backward with `tokens` tokens per worker."""
+    return _new(plan, _desc(plan, EmbedDesc, "dqgan_embed_bytes", offset, vocab, width, tokens, 1.0,
+                            _type(dtype, "dtype"), INDEX_TYPES[index_dtype], 0)[1])
 
 
 def embed_backward(plan, tokens, dout, G, vocab, workspace, offset=0, scale=1.0, add=False, stream=None):
     """The table's part of G [M][ld]: row v is scale * the sum of dout over the
     tokens that are v, 0 for those that do not occur; with `add` the sums are
     added to what is there."""
-    n = _rows(plan, dout, "dout", True)
-    d = EmbedDesc(offset, vocab, dout.shape[2], n, scale, _type(dout.dtype, "dout"), 0, 0)
-    tok = _like(plan, tokens, "tokens", (plan.M, n), tuple(INDEX_TYPES))
-    d.index_type = INDEX_TYPES.get(getattr(tokens, "dtype", None), 0)
-    ws = _workspace(plan, workspace, _bytes("dqgan_embed_bytes", plan, d))
-    _check("dqgan_embed_backward", load().dqgan_embed_backward(plan.handle, ctypes.byref(d), tok,
-                                                               _like(plan, dout, "dout", dout.shape, tuple(TYPES)),
-                                                               plan._mat(G, "G"), int(add), ws, _stream(stream)))
+    d, need, tok = _embed(plan, tokens, dout, "dout", vocab, offset, scale)
+    _check("dqgan_embed_backward", load().dqgan_embed_backward(plan.handle, d, tok,
+                                                               _like(plan, dout, "dout", dout.shape, TYPES),
+                                                               plan._mat(G, "G"), int(add),
+                                                               _workspace(plan, workspace, need), _on(plan, stream)))
 
 
 # ---------------------------------------------------------------------------
 # layer norm
 
 
-def _norm_desc(plan, x, gamma, beta, eps):
-    n = _rows(plan, x, "x", True)
-    return NormDesc(-1 if gamma is None else gamma, -1 if beta is None else beta, x.shape[2], n, eps,
-                    _type(x.dtype, "x"), 0)
+def _norm(plan, tokens, width, dtype, name, gamma, beta, eps):
+    return _desc(plan, NormDesc, "dqgan_norm_bytes", -1 if gamma is None else gamma, -1 if beta is None else beta, width,
+                 tokens, eps, _type(dtype, name), 0)
 
 
 def norm_forward(plan, x, P, y, stats=None, gamma=0, beta=None, eps=1e-5, stream=None):
@@ -173,36 +196,35 @@ def norm_forward(plan, x, P, y, stats=None, gamma=0, beta=None, eps=1e-5, stream
     bias at `gamma` and `beta` of each worker's row of P (None: without).
     stats [M][tokens][2] float32 takes mean and rstd for norm_backward; y may
     be x."""
-    d = _norm_desc(plan, x, gamma, beta, eps)
+    shape = _shape(plan, x, "x", 3)
+    d, _ = _norm(plan, shape[1], shape[2], x.dtype, "x", gamma, beta, eps)
     p, ldp = _params(plan, P)
     same = (x.dtype,)
     _check("dqgan_norm_forward",
-           load().dqgan_norm_forward(plan.handle, ctypes.byref(d), _like(plan, x, "x", x.shape, same), p, ldp,
-                                     _like(plan, y, "y", x.shape, same),
-                                     _like(plan, stats, "stats", x.shape[:2] + (2,), F32), _stream(stream)))
+           load().dqgan_norm_forward(plan.handle, d, _like(plan, x, "x", shape, same), p, ldp,
+                                     _like(plan, y, "y", shape, same),
+                                     _like(plan, stats, "stats", (shape[0], shape[1], 2), F32), _on(plan, stream)))
 
 
 def norm_workspace(plan, tokens, width, dtype, gamma=0, beta=None):
     """A workspace for norm_backward of these sizes (None if it needs none)."""
-    d = NormDesc(-1 if gamma is None else gamma, -1 if beta is None else beta, width, tokens, 0.0,
-                 _type(dtype, "dtype"), 0)
-    return _new(plan, _bytes("dqgan_norm_bytes", plan, d))
+    return _new(plan, _norm(plan, tokens, width, dtype, "dtype", gamma, beta, 0.0)[1])
 
 
 def norm_backward(plan, x, dy, P, stats, dx, G, workspace, gamma=0, beta=None, add=False, stream=None):
     """dx (None: not wanted; it may be dy), and the sums over a worker's tokens
     of dy * (x - mean) * rstd and of dy into its row of G at `gamma` and
     `beta`; with `add` added to what is there."""
-    d = _norm_desc(plan, x, gamma, beta, 0.0)
+    shape = _shape(plan, x, "x", 3)
+    d, need = _norm(plan, shape[1], shape[2], x.dtype, "x", gamma, beta, 0.0)
     p, ldp = _params(plan, P)
     same = (x.dtype,)
-    ws = _workspace(plan, workspace, _bytes("dqgan_norm_bytes", plan, d))
     _check("dqgan_norm_backward",
-           load().dqgan_norm_backward(plan.handle, ctypes.byref(d), _like(plan, x, "x", x.shape, same),
-                                      _like(plan, dy, "dy", x.shape, same), p, ldp,
-                                      _like(plan, stats, "stats", x.shape[:2] + (2,), F32),
-                                      _like(plan, dx, "dx", x.shape, same), plan._mat(G, "G"), int(add), ws,
-                                      _stream(stream)))
+           load().dqgan_norm_backward(plan.handle, d, _like(plan, x, "x", shape, same),
+                                      _like(plan, dy, "dy", shape, same), p, ldp,
+                                      _like(plan, stats, "stats", (shape[0], shape[1], 2), F32),
+                                      _like(plan, dx, "dx", shape, same), plan._mat(G, "G"), int(add),
+                                      _workspace(plan, workspace, need), _on(plan, stream)))
 
 
 # ---------------------------------------------------------------------------
@@ -210,21 +232,24 @@ def norm_backward(plan, x, dy, P, stats, dx, G, workspace, gamma=0, beta=None, a
 
 
 def _distill(plan, z, val, idx, weight, vocab, temperature):
-    """Descriptor and the pointers that every form of the loss takes."""
-    n = _rows(plan, z, "z", True)
+    """Descriptor, workspace, the pointers that every form of the loss takes,
+    and [M][tokens]."""
+    shape = _shape(plan, z, "z", 3)
+    rows = shape[:2]
     if not isinstance(val, torch.Tensor) or val.dim() != 3:
-        raise ValueError("val: expected a tensor of [%d][%d][k]" % (plan.M, n))
-    k = val.shape[2]
-    d = DistillDesc(z.shape[2] if vocab is None else vocab, z.shape[2], n, k, temperature, _type(z.dtype, "z"), 0)
-    return d, (_like(plan, z, "z", z.shape, tuple(TYPES)), _like(plan, val, "val", (plan.M, n, k), F32),
-               _like(plan, idx, "idx", (plan.M, n, k), U32), _like(plan, weight, "weight", (plan.M, n), F32))
+        raise ValueError("val: expected a tensor of [%d][%d][k]" % rows)
+    sent = (rows[0], rows[1], val.shape[2])
+    d, need = _desc(plan, DistillDesc, "dqgan_distill_bytes", shape[2] if vocab is None else vocab, shape[2], rows[1],
+                    sent[2], temperature, _type(z.dtype, "z"), 0)
+    return d, need, (_like(plan, z, "z", shape, TYPES), _like(plan, val, "val", sent, F32),
+                     _like(plan, idx, "idx", sent, U32), _like(plan, weight, "weight", rows, F32)), rows
 
 
 def distill_workspace(plan, tokens, vocab, k, dtype, ld=None):
     """A workspace for distill_forward and distill_fused of these sizes (None
     if they need none)."""
-    d = DistillDesc(vocab, vocab if ld is None else ld, tokens, k, 1.0, _type(dtype, "dtype"), 0)
-    return _new(plan, _bytes("dqgan_distill_bytes", plan, d))
+    return _new(plan, _desc(plan, DistillDesc, "dqgan_distill_bytes", vocab, vocab if ld is None else ld, tokens, k, 1.0,
+                            _type(dtype, "dtype"), 0)[1])
 
 
 def distill_forward(plan, z, val, idx, weight, loss, stats, vocab=None, workspace=None, temperature=1.0, stream=None):
@@ -233,30 +258,28 @@ def distill_forward(plan, z, val, idx, weight, loss, stats, vocab=None, workspac
     idx [M][tokens][k] (indices at or beyond vocab, as -1, are skipped):
     weight * T^2 * KL; weight [M][tokens] or None.  stats [M][tokens][2] is
     what distill_backward takes."""
-    d, args = _distill(plan, z, val, idx, weight, vocab, temperature)
-    rows = tuple(z.shape[:2])
-    ws = _workspace(plan, workspace, _bytes("dqgan_distill_bytes", plan, d))
+    d, need, args, rows = _distill(plan, z, val, idx, weight, vocab, temperature)
     _check("dqgan_distill_forward",
-           load().dqgan_distill_forward(plan.handle, ctypes.byref(d), *args, _like(plan, loss, "loss", rows, F32),
-                                        _like(plan, stats, "stats", rows + (2,), F32), ws, _stream(stream)))
+           load().dqgan_distill_forward(plan.handle, d, *args, _like(plan, loss, "loss", rows, F32),
+                                        _like(plan, stats, "stats", (rows[0], rows[1], 2), F32),
+                                        _workspace(plan, workspace, need), _on(plan, stream)))
 
 
 def distill_backward(plan, z, val, idx, weight, stats, dz, vocab=None, temperature=1.0, stream=None):
     """dz of distill_forward's loss; `weight` times the gradient that each loss
     receives takes its place as `weight`.  dz may be z."""
-    d, args = _distill(plan, z, val, idx, weight, vocab, temperature)
+    d, _, args, rows = _distill(plan, z, val, idx, weight, vocab, temperature)
     _check("dqgan_distill_backward",
-           load().dqgan_distill_backward(plan.handle, ctypes.byref(d), *args,
-                                         _like(plan, stats, "stats", tuple(z.shape[:2]) + (2,), F32),
-                                         _like(plan, dz, "dz", z.shape, (z.dtype,)), _stream(stream)))
+           load().dqgan_distill_backward(plan.handle, d, *args,
+                                         _like(plan, stats, "stats", (rows[0], rows[1], 2), F32),
+                                         _like(plan, dz, "dz", z.shape, (z.dtype,)), _on(plan, stream)))
 
 
 def distill_fused(plan, z, val, idx, weight, loss, dz, vocab=None, workspace=None, temperature=1.0, stream=None):
     """distill_forward and distill_backward in one call, the same bits; dz may
     be z."""
-    d, args = _distill(plan, z, val, idx, weight, vocab, temperature)
-    ws = _workspace(plan, workspace, _bytes("dqgan_distill_bytes", plan, d))
+    d, need, args, rows = _distill(plan, z, val, idx, weight, vocab, temperature)
     _check("dqgan_distill_fused",
-           load().dqgan_distill_fused(plan.handle, ctypes.byref(d), *args,
-                                      _like(plan, loss, "loss", tuple(z.shape[:2]), F32),
-                                      _like(plan, dz, "dz", z.shape, (z.dtype,)), ws, _stream(stream)))
+           load().dqgan_distill_fused(plan.handle, d, *args, _like(plan, loss, "loss", rows, F32),
+                                      _like(plan, dz, "dz", z.shape, (z.dtype,)), _workspace(plan, workspace, need),
+                                      _on(plan, stream)))
