@@ -2,24 +2,28 @@
 // its gradient, summed over sorted tokens into the worker's row of G.
 //
 // The gradient's launches:
-//   k_embed_sort   one workgroup per worker sorts its tokens (stable, so that
+//   k_embed_sort   sorts runs of kRun tokens, one workgroup each (stable, so that
 //                  equal ones stay in their order); the other workgroups of the
 //                  launch write the table's part of G as 0 meanwhile;
-//   k_embed_sum    chunks of kChunk sorted places, one wave per chunk and 512
-//                  channels.  A token whose places lie within a chunk has its row
-//                  written; one that runs across chunks leaves a partial sum in
-//                  each, so that a frequent token is as much work as a rare one;
+//   k_embed_merge  joins kFan sorted runs to one, as often as there is more than
+//                  one run: each token counts the smaller ones in the other runs;
+//   k_embed_sum    chunks of kChunk sorted places, one wave per chunk and 1 KB of
+//                  dout's rows.  It writes the rows of the tokens that begin in
+//                  its chunk and end there or in the next.  One that runs on
+//                  leaves a partial sum in each of its chunks, so that a frequent
+//                  token is as much work as a rare one;
 //   k_embed_join   sums those.
 #include "layers.hpp"
 
 namespace dq {
 namespace {
 
-constexpr int kChunk = 32;           // sorted places per wave of k_embed_sum
-constexpr int kSlab = 512;           // channels per wave
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kDigitMost = 9;        // bits of a sort digit: 512 counters for each of 16 waves
-constexpr int64_t kFillFloats = 16384;  // of G per workgroup
+constexpr int kChunk = 32;                 // sorted places per wave of k_embed_sum (at most 64)
+constexpr int kRun = 4096;                 // tokens per workgroup of k_embed_sort
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kEach = kRun / kSortThreads;
+constexpr int kDigitMost = 9;              // bits of a sort digit: 512 counters for each of 16 waves
+constexpr int kFan = 16;
+constexpr int64_t kFillFloats = 32768;     // of G per workgroup
 
 struct EmbedArgs {
     int64_t offset, V, D, N, ld;
@@ -50,95 +54,101 @@ __global__ __launch_bounds__(256) void k_embed_fwd(const I *tok, const float *P,
     }
 }
 
-// The sorted lists of one worker: token and place, with padded places as token V
-// behind all others.
-struct Lists {
-    uint32_t *key[2], *at[2];  // [M][N]: the passes go from one pair to the other
-};
-
+// A worker's tokens to sort: padded places count as token V, behind all others.
 template <typename I>
 __device__ __forceinline__ uint32_t key_of(const I *tok, int64_t i, int64_t V) {
     const I t = tok[i];
     return t >= 0 && static_cast<int64_t>(t) < V ? static_cast<uint32_t>(t) : static_cast<uint32_t>(V);
 }
 
-// Stable sort by digits from the lowest up.  A wave owns a contiguous run of
-// places and, of the counters [digit][wave], its own column.
+// Stable sort of one run by digits from the lowest up, in registers and LDS.  A
+// wave owns 256 consecutive places and, of the counters [digit][wave], its own
+// column; a lane finds the lanes of its wave with its digit by one ballot a bit.
 template <typename I>
-__device__ void sort_tokens(const I *tok, int64_t V, int64_t N, uint32_t *const key[2], uint32_t *const at[2], int bits,
-                            int passes) {
-    __shared__ uint32_t count[kSortWaves << kDigitMost];
+__device__ void sort_run(const I *tok, int64_t begin, int64_t N, int64_t V, int bits, int passes, uint32_t *key,
+                         uint32_t *at) {
+    __shared__ __align__(16) uint16_t count[kSortWaves << kDigitMost];
+    __shared__ uint32_t keys[kRun];
+    __shared__ uint16_t places[kRun];
     __shared__ uint32_t total[kSortWaves];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int64_t run = (N + kSortThreads - 1) / kSortThreads * 64;
-    const int64_t begin = wave * run < N ? wave * run : N, end = begin + run < N ? begin + run : N;
-    const int counters = kSortWaves << bits;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, mine = wave * 64 * kEach + lane;
+    const int each = (kSortWaves << bits) / kSortThreads;  // counters per thread
+    uint32_t k[kEach], rank[kEach];
+    uint16_t place[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int i = mine + 64 * j;
+        k[j] = begin + i < N ? key_of(tok, begin + i, V) : static_cast<uint32_t>(V);
+        place[j] = static_cast<uint16_t>(i);
+    }
     for (int p = 0; p < passes; ++p) {
-        const uint32_t *from_key = key[(p + 1) & 1], *from_at = at[(p + 1) & 1];
-        uint32_t *to_key = key[p & 1], *to_at = at[p & 1];
         const int shift = p * bits;
-        const uint32_t mask = (1u << bits) - 1;
-        for (int i = tid; i < counters; i += kSortThreads) count[i] = 0;
+        for (int i = tid; i < (kSortWaves << bits) / 2; i += kSortThreads) reinterpret_cast<uint32_t *>(count)[i] = 0;
         __syncthreads();
-        for (int64_t i = begin + lane; i < end; i += 64) {
-            const uint32_t k = p == 0 ? key_of(tok, i, V) : from_key[i];
-            atomicAdd(&count[((k >> shift & mask) * kSortWaves) + wave], 1u);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const uint32_t digit = k[j] >> shift & ((1u << bits) - 1);
+            uint64_t same = ~uint64_t(0);
+            for (int b = 0; b < bits; ++b) {
+                const bool set = digit >> b & 1;
+                const uint64_t with = __ballot(set);
+                same &= set ? with : ~with;
+            }
+            volatile uint16_t *slot = &count[digit * kSortWaves + wave];
+            const uint32_t first = *slot;
+            const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
+            if (before == 0) *slot = static_cast<uint16_t>(first + __popcll(same));
+            rank[j] = first + before;
         }
         __syncthreads();
         // exclusive sums over [digit][wave]
-        const int each = counters / kSortThreads;
         uint32_t sum = 0;
         for (int i = 0; i < each; ++i) sum += count[tid * each + i];
-        uint32_t upto = sum;
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t other = __shfl_up(upto, o);
-            if (lane >= o) upto += other;
-        }
+        const uint32_t upto = wave_prefix(sum);
         if (lane == 63) total[wave] = upto;
         __syncthreads();
-        uint32_t base = upto - sum;
-        for (int w = 0; w < wave; ++w) base += total[w];
+        const uint32_t totals = row_prefix(total[lane & (kSortWaves - 1)]);
+        uint32_t base = upto - sum + (wave > 0 ? __builtin_amdgcn_readlane(totals, wave > 0 ? wave - 1 : 0) : 0);
         for (int i = 0; i < each; ++i) {
             const uint32_t c = count[tid * each + i];
-            count[tid * each + i] = base;
+            count[tid * each + i] = static_cast<uint16_t>(base);
             base += c;
         }
         __syncthreads();
-        for (int64_t i0 = begin; i0 < end; i0 += 64) {
-            const int64_t i = i0 + lane;
-            const bool in = i < end;
-            const uint32_t k = !in ? 0 : p == 0 ? key_of(tok, i, V) : from_key[i];
-            const uint32_t where = p == 0 || !in ? static_cast<uint32_t>(i) : from_at[i];
-            const uint32_t digit = k >> shift & mask;
-            uint64_t same = __ballot(in);
-            for (int b = 0; b < bits; ++b) {
-                const uint64_t set = __ballot(digit >> b & 1);
-                same &= (digit >> b & 1) ? set : ~set;
-            }
-            if (in) {
-                uint32_t *slot = &count[digit * kSortWaves + wave];
-                const uint32_t first = *reinterpret_cast<volatile uint32_t *>(slot);
-                const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
-                if (before == 0) *reinterpret_cast<volatile uint32_t *>(slot) = first + __popcll(same);
-                to_key[first + before] = k;
-                to_at[first + before] = where;
-            }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const uint32_t to = count[(k[j] >> shift & ((1u << bits) - 1)) * kSortWaves + wave] + rank[j];
+            keys[to] = k[j];
+            places[to] = place[j];
         }
         __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            k[j] = keys[mine + 64 * j];
+            place[j] = places[mine + 64 * j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int64_t i = begin + mine + 64 * j;  // what lies beyond N came last and stays there
+        if (i < N) {
+            key[i] = k[j];
+            at[i] = static_cast<uint32_t>(begin + place[j]);
+        }
     }
 }
 
 template <typename I>
-__global__ __launch_bounds__(kSortThreads) void k_embed_sort(const I *tok, EmbedArgs a, int M, Lists l, int bits,
-                                                             int passes, int fills, float *G) {
-    if (static_cast<int>(blockIdx.x) < M) {
-        const int64_t at = static_cast<int64_t>(blockIdx.x) * a.N;
-        uint32_t *const keys[2] = {l.key[0] + at, l.key[1] + at}, *const ats[2] = {l.at[0] + at, l.at[1] + at};
-        sort_tokens(tok + at, a.V, a.N, keys, ats, bits, passes);
+__global__ __launch_bounds__(kSortThreads) void k_embed_sort(const I *tok, EmbedArgs a, int runs, int sorts, int bits,
+                                                             int passes, uint32_t *key, uint32_t *at, int fills, float *G) {
+    if (static_cast<int>(blockIdx.x) < sorts) {
+        const int64_t first = static_cast<int64_t>(blockIdx.x / runs) * a.N;
+        sort_run(tok + first, static_cast<int64_t>(blockIdx.x % runs) * kRun, a.N, a.V, bits, passes, key + first,
+                 at + first);
         return;
     }
     // the table's part of G, from a 16-byte boundary on in vectors
-    const int64_t b = blockIdx.x - M, m = b / fills, len = a.V * a.D;
+    const int64_t b = blockIdx.x - sorts, m = b / fills, len = a.V * a.D;
     float *to = G + m * a.ld + a.offset;
     const int64_t head = len < ((4 - (a.offset & 3)) & 3) ? len : ((4 - (a.offset & 3)) & 3);
     const int64_t quads = (len - head) / 4, each = (quads + fills - 1) / fills;
@@ -151,100 +161,272 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const I *tok, Embed
     }
 }
 
-__device__ __forceinline__ void put_row(float *to, int64_t n, f32x8 s, float scale, bool add) {
-    if (n <= 0) return;
-    f32x8 f = 0.0f;
-    if (add) f = load8(to, n);
+// Runs of `len` places (at least a workgroup's 256) to runs of kFan * len: a
+// token's new place is its place in its run plus, for each other run, how many of
+// its tokens come before.  A wave holds 64 neighbours of a sorted run: first its
+// lanes search for its first and its last token, four lanes a run, each of which
+// looks at one of the four places that cut what is left in five; the other
+// tokens' counts lie between those two, most often a few places apart.  Every
+// step waits for memory, so searches go side by side.
+__global__ __launch_bounds__(256) void k_embed_merge(const uint32_t *key, const uint32_t *at, int N, int len,
+                                                     uint32_t *to_key, uint32_t *to_at) {
+    static_assert(kFan == 16, "four lanes a run");
+    const int first = static_cast<int>(blockIdx.x) * 256, i = first + threadIdx.x, lane = threadIdx.x & 63;
+    const int64_t m = blockIdx.y;
+    key += m * N;
+    at += m * N;
+    const int run = first / len, group = run / kFan * kFan;
+    const bool in = i < N;
+    const uint32_t k = key[in ? i : N - 1], where = at[in ? i : N - 1];
+    uint32_t ends[2] = {0, 0};  // counts of the wave's first and last token in run group + lane % 16
+    {
+        const int r = lane & 15, j = lane >> 4;
+        const int64_t begin = static_cast<int64_t>(group + r) * len;
+        const uint32_t here = begin >= N || group + r == run ? 0 : static_cast<uint32_t>(N - begin < len ? N - begin : len);
+        const uint32_t mine[2] = {static_cast<uint32_t>(__builtin_amdgcn_readlane(k, 0)) + (group + r < run),
+                                  static_cast<uint32_t>(__builtin_amdgcn_readlane(k, 63)) + (group + r < run)};
+        uint32_t left[2] = {here, here};  // the count is in [ends, ends + left]
+        while (__ballot((left[0] | left[1]) != 0) != 0) {
+            bool before[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = add ? f[i] + s[i] * scale : s[i] * scale;
-    store8(to, n, f);
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t cut = ends[e] + static_cast<uint32_t>(uint64_t(j + 1) * (left[e] + 1) / 5);
+                before[e] = cut <= ends[e] || key[begin + cut - 1] < mine[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint64_t votes = __ballot(before[e]) >> r;  // bits 0, 16, 32, 48: this run's four
+                const int yes = (votes & 1) + (votes >> 16 & 1) + (votes >> 32 & 1) + (votes >> 48 & 1);
+                const uint32_t n = left[e], low = ends[e];
+                if (yes > 0) ends[e] = low + static_cast<uint32_t>(uint64_t(yes) * (n + 1) / 5);
+                const uint32_t high = yes < 4 ? low + static_cast<uint32_t>(uint64_t(yes + 1) * (n + 1) / 5) - 1 : low + n;
+                left[e] = high - ends[e];
+            }
+        }
+    }
+    uint32_t less[kFan], most[kFan], width = 0;
+#pragma unroll
+    for (int r = 0; r < kFan; ++r) {
+        less[r] = __builtin_amdgcn_readlane(ends[0], r);
+        most[r] = __builtin_amdgcn_readlane(ends[1], r);
+        width = most[r] - less[r] > width ? most[r] - less[r] : width;
+    }
+    for (int step = width == 0 ? 0 : 1 << (31 - __builtin_clz(width)); step > 0; step >>= 1) {
+#pragma unroll
+        for (int r = 0; r < kFan; ++r) {
+            const uint32_t upto = less[r] + step;
+            // equal tokens of earlier runs come before, of later ones behind
+            if (upto <= most[r] && key[static_cast<int64_t>(group + r) * len + upto - 1] < k + (group + r < run))
+                less[r] = upto;
+        }
+    }
+    int64_t to = static_cast<int64_t>(group) * len + (i - run * len);
+#pragma unroll
+    for (int r = 0; r < kFan; ++r) to += less[r];
+    if (!in) return;
+    to_key[m * N + to] = k;
+    to_at[m * N + to] = where;
 }
 
+// A lane's channels: sixteen bytes of dout (`whole`), and one of the last D % kPer
+// in the first lanes of the last slab (`tail`).  `from` and `from_tail` are places
+// within the row for the lanes without any too, so that loads need no branch.
+template <typename T>
+struct Channels {
+    typedef typename Vec16<T>::wide Wide;
+    static constexpr int kPer = Vec16<T>::kPer;
+    int64_t c, ct, from, from_tail;  // first channel, tail channel
+    bool whole, tail, some_whole, some_tail;
+    __device__ __forceinline__ Channels(int64_t D, int slab, int slabs, int width, int lane) {
+        const int64_t vectors = D / kPer, q = static_cast<int64_t>(slab) * width + lane;
+        whole = lane < width && q < vectors;
+        c = kPer * q;
+        ct = kPer * vectors + lane;
+        tail = slab == slabs - 1 && ct < D;
+        some_whole = vectors > 0;
+        some_tail = slab == slabs - 1 && kPer * vectors < D;
+        from = whole ? c : 0;
+        from_tail = tail ? ct : D - 1;
+    }
+    __device__ __forceinline__ void put(float *to, Wide s, float t, float scale, bool add) const {
+        if (whole) {
+            Wide f = s * scale;
+            if (add) f += load_floats<T>(to + c);
+            store_floats<T>(to + c, f);
+        }
+        if (tail) to[ct] = add ? to[ct] + t * scale : t * scale;
+    }
+    __device__ __forceinline__ void leave(float *to, Wide s, float t) const {
+        if (whole) store_floats<T>(to + c, s);
+        if (tail) to[ct] = t;
+    }
+};
+
+constexpr int kBatch = 8;
 template <typename T>
 __global__ __launch_bounds__(256) void k_embed_sum(const uint32_t *key, const uint32_t *at, const T *dout, EmbedArgs a,
-                                                   int64_t chunks, int slabs, float *part, float *G, bool add) {
+                                                   int64_t chunks, int slabs, int width, float *part, float *G, bool add) {
+    static_assert(2 * kChunk <= 64, "a lane for each place of a chunk and the next");
     const int64_t m = blockIdx.y, task = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (task >= chunks * slabs) return;
-    const int64_t chunk = task / slabs, c = (task % slabs) * kSlab + 8 * (threadIdx.x & 63), rest = a.D - c;
-    const int64_t e0 = chunk * kChunk, e1 = e0 + kChunk < a.N ? e0 + kChunk : a.N;
-    const int n = static_cast<int>(e1 - e0);
+    const int lane = threadIdx.x & 63;
+    const int64_t chunk = task / slabs;
+    const Channels<T> ch(a.D, static_cast<int>(task % slabs), slabs, width, lane);
+    const int64_t e0 = chunk * kChunk;
     key += m * a.N;
     at += m * a.N;
     dout += m * a.N * a.D;
     G += m * a.ld + a.offset;
     part += (m * chunks + chunk) * 2 * a.D;
     const uint32_t V = static_cast<uint32_t>(a.V);
-    const uint32_t before = e0 > 0 ? key[e0 - 1] : V, after = e1 < a.N ? key[e1] : V;
-    f32x8 s = 0.0f;
-    int from = 0;
-    for (int e = 0; e < n; ++e) {
-        const uint32_t k = key[e0 + e];
-        if (k == V) break;
-        if (rest > 0) {
-            const f32x8 f = load8(dout + static_cast<int64_t>(at[e0 + e]) * a.D + c, rest);
+    // lane i: place e0 + i of this chunk and the next, and whether its token ends there
+    const uint32_t k = e0 + lane < a.N ? key[e0 + lane] : V;
+    const uint32_t where = e0 + lane < a.N ? at[e0 + lane] : 0;
+    const uint32_t before = e0 > 0 ? key[e0 - 1] : V;
+    const uint32_t earlier = e0 > kChunk ? key[e0 - kChunk - 1] : V;  // the last place before the chunk before
+    const uint32_t behind = e0 + 2 * kChunk < a.N ? key[e0 + 2 * kChunk] : V;
+    uint32_t next = __shfl_down(k, 1);
+    if (lane == 2 * kChunk - 1) next = behind;
+    const uint64_t ends = __ballot(k != next);
+    const int valid = __popcll(__ballot(k != V));  // padded places come last
+    const uint32_t head = __builtin_amdgcn_readlane(k, 0);
+    // places of the token that began in an earlier chunk, and whether it was that chunk's to finish
+    const int led = head != V && head == before ? (ends != 0 ? __ffsll(static_cast<long long>(ends)) : 65) : 0;
+    const bool finished = led <= kChunk && earlier != head;
+    int first = led > 0 && finished ? led : 0;
+    bool leading = led > 0 && !finished;  // its partial sum comes first
+    // to the end of the last token that begins here, if that is in sight
+    int n = valid < kChunk ? valid : kChunk;
+    if (n == kChunk && !(ends >> (kChunk - 1) & 1)) {
+        const bool mine = !(leading && led > kChunk);  // it begins here
+        const uint64_t later = ends >> kChunk;
+        if (mine && later != 0) n = kChunk + __ffsll(static_cast<long long>(later));
+    }
+    typename Vec16<T>::wide s = 0.0f;
+    float t = 0.0f;
+    for (int b = first; b < n; b += kBatch) {
+        const T *row[kBatch];
+        typename Vec16<T>::type raw[kBatch];
+        typename Bits<T>::type last[kBatch];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] += f[i];
+        for (int u = 0; u < kBatch; ++u) {
+            const int e = b + u < n ? b + u : b;  // beyond n: this batch's first row once more
+            row[u] = dout + static_cast<int64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(where, e))) * a.D;
         }
-        const uint32_t next = e + 1 < n ? key[e0 + e + 1] : after;
-        if (e + 1 < n && next == k) continue;
-        const bool began = from == 0 && before == k, goes_on = e + 1 == n && next == k;
-        if (!began && !goes_on)
-            put_row(G + static_cast<int64_t>(k) * a.D + c, rest, s, a.scale, add);
-        else
-            store8(part + (began ? 0 : a.D) + c, rest, s);
-        s = 0.0f;
-        from = e + 1;
+        if (ch.some_whole) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) raw[u] = load16(row[u] + ch.from);
+        }
+        if (ch.some_tail) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) last[u] = load_bits(row[u] + ch.from_tail);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (b + u >= n) break;
+            if (ch.some_whole) s += widen<T>(raw[u]);
+            if (ch.some_tail) t += widen_bits<T>(last[u]);
+            const bool end = ends >> (b + u) & 1;
+            if (!end && b + u + 1 < n) continue;
+            if (!leading && end)
+                ch.put(G + static_cast<int64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(k, b + u))) * a.D, s, t,
+                       a.scale, add);
+            else
+                ch.leave(part + (leading ? 0 : a.D), s, t);
+            s = 0.0f;
+            t = 0.0f;
+            leading = false;
+        }
     }
 }
 
-// A token that runs on beyond the chunk it begins in: that chunk's second
-// partial sum and the first ones of those that follow.
-template <int W>
-__global__ __launch_bounds__(64 * W) void k_embed_join(const uint32_t *key, EmbedArgs a, int64_t chunks, int slabs,
-                                                       const float *part, float *G, bool add) {
-    __shared__ float sums[W > 1 ? W - 1 : 1][64][8];
-    const int64_t m = blockIdx.y, chunk = static_cast<int64_t>(blockIdx.x) / slabs;
-    key += m * a.N;
-    const uint32_t V = static_cast<uint32_t>(a.V);
-    const int64_t e0 = chunk * kChunk, e1 = e0 + kChunk;
-    if (e1 >= a.N) return;
-    const uint32_t k = key[e1 - 1];
-    if (k == V || key[e1] != k) return;
-    if (e0 > 0 && key[e0 - 1] == k) return;
-    int64_t lo = e1, hi = a.N;  // key[lo] == k, the first other key is at or below hi
-    while (hi - lo > 1) {
-        const int64_t mid = lo + (hi - lo) / 2;
-        if (key[mid] == k)
-            lo = mid;
-        else
-            hi = mid;
-    }
-    const int64_t last = lo / kChunk;
+// Tokens that run on beyond the chunk after the one they begin in: that chunk's
+// second partial sum and the first ones of those that follow, in this order.  One workgroup per
+// kJoinChunks chunks and slab: its waves look at the chunks' borders, one lane a
+// chunk, then take such tokens in turn; one of many chunks is shared out among
+// them.
+constexpr int kJoinWaves = 8, kJoinChunks = 16, kMany = 2 * kBatch;
+template <typename T>
+__global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(const uint32_t *key, EmbedArgs a, int64_t chunks, int slabs,
+                                                                int width, const float *part, float *G, bool add) {
+    __shared__ float sums[kJoinWaves][64][Vec16<T>::kPer + 1], tails[kJoinWaves][64];
+    typedef typename Vec16<T>::wide Wide;
+    const int64_t m = blockIdx.y, from = static_cast<int64_t>(blockIdx.x / slabs) * kJoinChunks;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t c = (blockIdx.x % slabs) * kSlab + 8 * lane, rest = a.D - c;
-    part += m * chunks * 2 * a.D + c;
-    // each wave a contiguous share of the partial sums
-    const int64_t each = (last - chunk + W - 1) / W, first = chunk + 1 + wave * each;
-    const int64_t upto = first + each < last + 1 ? first + each : last + 1;
-    f32x8 s = 0.0f;
-    if (wave == 0) s = load8(part + (2 * chunk + 1) * a.D, rest);
-    for (int64_t b = first; b < upto; ++b) {
-        const f32x8 f = load8(part + 2 * b * a.D, rest);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] += f[i];
+    key += m * a.N;
+    G += m * a.ld + a.offset;
+    part += m * chunks * 2 * a.D;
+    const uint32_t V = static_cast<uint32_t>(a.V);
+    const int64_t e0 = (from + lane) * kChunk, e1 = e0 + kChunk;
+    bool begins = false;  // a token begins in chunk from + lane and runs on
+    uint32_t k = V;
+    if (lane < kJoinChunks && e1 < a.N) {
+        k = key[e1 - 1];
+        begins = e1 + kChunk < a.N && k != V && key[e1 + kChunk] == k && !(e0 > 0 && key[e0 - 1] == k);
     }
-    if (W > 1) {
-        if (wave > 0) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sums[wave - 1][lane][i] = s[i];
+    const Channels<T> ch(a.D, static_cast<int>(blockIdx.x % slabs), slabs, width, lane);
+    uint64_t todo = __ballot(begins);
+    for (int turn = 0; todo != 0; todo &= todo - 1, ++turn) {
+        const int l = __ffsll(static_cast<long long>(todo)) - 1;
+        const int64_t chunk = from + l;
+        const uint32_t token = __builtin_amdgcn_readlane(k, l);
+        // chunks that begin with this token: 64 looked at in one go
+        int64_t last = chunk + 1;
+        for (;;) {
+            const int64_t first = (last + lane) * kChunk;
+            const uint64_t others = ~__ballot(first < a.N && key[first < a.N ? first : 0] == token);
+            if (others != 0) {
+                last += __ffsll(static_cast<long long>(others)) - 1;
+                break;
+            }
+            last += 64;
         }
-        __syncthreads();
-        if (wave > 0) return;
-        for (int w = 0; w < W - 1; ++w)
+        const int64_t n = last - chunk - 1;
+        const bool shared = n > kMany;  // the same for the whole workgroup
+        if (!shared && turn % kJoinWaves != wave) continue;
+        const int64_t each = shared ? (n + kJoinWaves - 1) / kJoinWaves : n;
+        const int64_t first = chunk + 1 + (shared ? wave * each : 0), upto = first + each < last ? first + each : last;
+        Wide s = 0.0f;
+        float t = 0.0f;
+        if (!shared || wave == 0) {
+            const float *p = part + (2 * chunk + 1) * a.D;
+            if (ch.whole) s = load_floats<T>(p + ch.c);
+            if (ch.tail) t = p[ch.ct];
+        }
+        for (int64_t b = first; b < upto; b += kBatch) {
+            const float *p = part + 2 * b * a.D;
+            if (ch.some_whole) {
+                Wide f[kBatch];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] += sums[w][lane][i];
+                for (int u = 0; u < kBatch; ++u) f[u] = load_floats<T>(p + (b + u < upto ? 2 * u * a.D : 0) + ch.from);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+                    if (b + u < upto) s += f[u];
+            }
+            if (ch.some_tail) {
+                float f[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) f[u] = p[(b + u < upto ? 2 * u * a.D : 0) + ch.from_tail];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+                    if (b + u < upto) t += f[u];
+            }
+        }
+        if (shared) {
+            __syncthreads();  // the one before has been read
+#pragma unroll
+            for (int i = 0; i < ch.kPer; ++i) sums[wave][lane][i] = s[i];
+            tails[wave][lane] = t;
+            __syncthreads();
+            if (wave != 0) continue;
+            for (int w = 1; w < kJoinWaves; ++w) {
+#pragma unroll
+                for (int i = 0; i < ch.kPer; ++i) s[i] += sums[w][lane][i];
+                t += tails[w][lane];
+            }
+        }
+        ch.put(G + static_cast<int64_t>(token) * a.D, s, t, a.scale, add);
     }
-    put_row(G + m * a.ld + a.offset + static_cast<int64_t>(k) * a.D + c, rest, s, a.scale, add);
 }
 
 // ---------------------------------------------------------------------------
@@ -252,7 +434,12 @@ __global__ __launch_bounds__(64 * W) void k_embed_join(const uint32_t *key, Embe
 constexpr int64_t kMostGroups = int64_t(1) << 24;  // of 256 threads in a launch's first dimension: below 2^32 threads
 
 int64_t chunks_of(int64_t N) { return ceil_div(N, kChunk); }
-int slabs_of(int64_t D) { return static_cast<int>(ceil_div(D, kSlab)); }
+// The vectors of a row in equal shares of up to 64, one per wave.
+int slabs_of(int64_t D, int per) {
+    const int64_t s = ceil_div(D / per, 64);
+    return static_cast<int>(s < 1 ? 1 : s);
+}
+int width_of(int64_t D, int per) { return static_cast<int>(ceil_div(D / per, slabs_of(D, per))); }
 
 dqgan_status check(dqgan_plan P, const dqgan_embed_desc *d) {
     if (!P || !d) return DQGAN_EINVAL;
@@ -261,7 +448,7 @@ dqgan_status check(dqgan_plan P, const dqgan_embed_desc *d) {
     if (d->offset < 0 || d->offset >= n || d->vocab > (n - d->offset) / d->width) return DQGAN_EINVAL;
     if (!tokens_ok(P, d->tokens) || !type_ok(d->type) || d->reserved != 0 || !isfinite(d->scale)) return DQGAN_EINVAL;
     if (d->index_type != DQGAN_I32 && d->index_type != DQGAN_I64) return DQGAN_EINVAL;
-    if (chunks_of(d->tokens) * slabs_of(d->width) > kMostGroups) return DQGAN_EINVAL;
+    if (chunks_of(d->tokens) * slabs_of(d->width, 4) > kMostGroups) return DQGAN_EINVAL;
     return DQGAN_OK;
 }
 
@@ -279,8 +466,10 @@ void with_index(int32_t type, F &&f) {
 
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
-// The workspace: two pairs of lists, then the partial sums.
+// The workspace: lists of tokens and of their places (two pairs where runs are
+// merged), then the partial sums.
 size_t list_bytes(int64_t M, int64_t N) { return round256(sizeof(uint32_t) * static_cast<size_t>(M * N)); }
+int pairs_of(int64_t N) { return N > kRun ? 2 : 1; }
 
 }  // namespace
 }  // namespace dq
@@ -321,8 +510,8 @@ dqgan_status dqgan_embed_bytes(dqgan_plan P, const dqgan_embed_desc *d, size_t *
     if (!bytes) return DQGAN_EINVAL;
     const int64_t M = P->desc.M;
     *bytes = d->tokens == 0 ? 0
-                            : 4 * list_bytes(M, d->tokens) + sizeof(float) * 2 *
-                                                                 static_cast<size_t>(M * chunks_of(d->tokens)) * d->width;
+                            : 2 * pairs_of(d->tokens) * list_bytes(M, d->tokens) +
+                                  sizeof(float) * 2 * static_cast<size_t>(M * chunks_of(d->tokens)) * d->width;
     return DQGAN_OK;
 }
 
@@ -338,13 +527,13 @@ dqgan_status dqgan_embed_backward(dqgan_plan P, const dqgan_embed_desc *d, const
     hipStream_t st = static_cast<hipStream_t>(stream);
     const EmbedArgs a = args(P, d);
     const int64_t M = P->desc.M;
-    Lists l{};
-    if (any)
-        for (int i = 0; i < 2; ++i) {
-            l.key[i] = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + (2 * i) * list_bytes(M, a.N));
-            l.at[i] = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + (2 * i + 1) * list_bytes(M, a.N));
-        }
-    float *part = reinterpret_cast<float *>(static_cast<char *>(workspace) + 4 * list_bytes(M, a.N));
+    const size_t list = list_bytes(M, a.N);
+    uint32_t *key[2], *at[2];
+    for (int i = 0; i < 2; ++i) {
+        key[i] = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + 2 * i * list);
+        at[i] = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + (2 * i + 1) * list);
+    }
+    float *part = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * pairs_of(a.N) * list);
     int bits = 1;  // of the largest key, V
     while ((a.V >> bits) != 0) ++bits;
     const int passes = (bits + kDigitMost - 1) / kDigitMost;
@@ -352,25 +541,30 @@ dqgan_status dqgan_embed_backward(dqgan_plan P, const dqgan_embed_desc *d, const
     if (digit < 6) digit = 6;  // 1024 counters at least: one per thread
     const int64_t want = ceil_div(a.V * a.D, kFillFloats), most = kMostGroups / 8 / M;
     const int fills = add ? 0 : static_cast<int>(want < most ? want : most);
-    const int sorts = any ? static_cast<int>(M) : 0;
-    const uint32_t groups = static_cast<uint32_t>(sorts + M * fills);
+    const int runs = static_cast<int>(ceil_div(a.N, kRun)), sorts = static_cast<int>(M * runs);
+    const int64_t groups = sorts + M * fills;
     if (groups == 0) return DQGAN_OK;
     with_index(d->index_type, [&](auto i) {
         using I = decltype(i);
-        k_embed_sort<I><<<groups, kSortThreads, 0, st>>>(static_cast<const I *>(tok), a, sorts, l, digit, passes, fills, G);
+        k_embed_sort<I><<<static_cast<uint32_t>(groups), kSortThreads, 0, st>>>(
+            static_cast<const I *>(tok), a, runs, sorts, digit, passes, key[0], at[0], fills, G);
     });
     if (!any) return launched();
-    const uint32_t *key = l.key[(passes - 1) & 1], *at = l.at[(passes - 1) & 1];
+    int now = 0;
+    for (int64_t len = kRun; len < a.N; len *= kFan, now ^= 1)
+        k_embed_merge<<<dim3(static_cast<uint32_t>(ceil_div(a.N, 256)), static_cast<uint32_t>(M)), 256, 0, st>>>(
+            key[now], at[now], static_cast<int>(a.N), static_cast<int>(len), key[now ^ 1], at[now ^ 1]);
     const int64_t chunks = chunks_of(a.N);
-    const int slabs = slabs_of(a.D);
-    const dim3 grid(static_cast<uint32_t>(ceil_div(chunks * slabs, 4)), static_cast<uint32_t>(M));
     with_type(d->type, [&](auto t) {
         using T = decltype(t);
-        k_embed_sum<T><<<grid, 256, 0, st>>>(key, at, static_cast<const T *>(dout), a, chunks, slabs, part, G, add != 0);
+        const int slabs = slabs_of(a.D, Vec16<T>::kPer), width = width_of(a.D, Vec16<T>::kPer);
+        const uint32_t my = static_cast<uint32_t>(M);
+        k_embed_sum<T><<<dim3(static_cast<uint32_t>(ceil_div(chunks * slabs, 4)), my), 256, 0, st>>>(
+            key[now], at[now], static_cast<const T *>(dout), a, chunks, slabs, width, part, G, add != 0);
+        if (chunks > 2)
+            k_embed_join<T><<<dim3(static_cast<uint32_t>(ceil_div(chunks, kJoinChunks) * slabs), my), 64 * kJoinWaves, 0, st>>>(
+                key[now], a, chunks, slabs, width, part, G, add != 0);
     });
-    if (chunks > 1)
-        k_embed_join<4><<<dim3(static_cast<uint32_t>(chunks * slabs), static_cast<uint32_t>(M)), 256, 0, st>>>(
-            key, a, chunks, slabs, part, G, add != 0);
     return launched();
 }
 

@@ -78,6 +78,44 @@ struct Vec16 {
     typedef float wide __attribute__((ext_vector_type(16 / sizeof(T))));
 };
 
+// An element's bits: a load that is not converted where it is issued.
+template <typename T>
+struct Bits {
+    typedef uint16_t type;
+};
+template <>
+struct Bits<float> {
+    typedef uint32_t type;
+};
+template <typename T>
+__device__ __forceinline__ typename Bits<T>::type load_bits(const T *p) {
+    return *reinterpret_cast<const typename Bits<T>::type *>(p);
+}
+template <typename T>
+__device__ __forceinline__ float widen_bits(typename Bits<T>::type b) {
+    return static_cast<float>(__builtin_bit_cast(T, b));
+}
+
+template <typename T>
+__device__ __forceinline__ typename Vec16<T>::type load16(const T *p) {
+    return *reinterpret_cast<const typename Vec16<T>::packed *>(p);
+}
+template <typename T>
+__device__ __forceinline__ typename Vec16<T>::wide widen(typename Vec16<T>::type v) {
+    return __builtin_convertvector(v, typename Vec16<T>::wide);
+}
+// As many floats of a parameter's row (a lane's channels of Vec16<T>).
+template <typename T>
+__device__ __forceinline__ typename Vec16<T>::wide load_floats(const float *p) {
+    typedef float packed __attribute__((ext_vector_type(16 / sizeof(T)), aligned(4)));
+    return *reinterpret_cast<const packed *>(p);
+}
+template <typename T>
+__device__ __forceinline__ void store_floats(float *p, typename Vec16<T>::wide v) {
+    typedef float packed __attribute__((ext_vector_type(16 / sizeof(T)), aligned(4)));
+    *reinterpret_cast<packed *>(p) = v;
+}
+
 // p[0..8), of which n are there; the others come as `fill`.
 template <typename T>
 __device__ __forceinline__ f32x8 load8(const T *p, int64_t n, float fill = 0.0f) {
@@ -129,6 +167,25 @@ __device__ __forceinline__ float wave_max(float x) {
     x = fmaxf(x, dpp_or<0x142, 0xA>(x, x));
     x = fmaxf(x, dpp_or<0x143, 0xC>(x, x));
     return lane63(x);
+}
+
+// Sum over this lane and those before it in its row of 16, and in the wave.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_zero(uint32_t x) {
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ uint32_t row_prefix(uint32_t x) {
+    x += dpp_zero<0x111, 0xF>(x);
+    x += dpp_zero<0x112, 0xF>(x);
+    x += dpp_zero<0x114, 0xF>(x);
+    x += dpp_zero<0x118, 0xF>(x);
+    return x;
+}
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t x) {
+    x = row_prefix(x);
+    x += dpp_zero<0x142, 0xA>(x);
+    x += dpp_zero<0x143, 0xC>(x);
+    return x;
 }
 
 // Sum and maximum over groups of W consecutive lanes (4, 8 or 16), in each.

@@ -1,6 +1,6 @@
 """Embedding lookup and its gradient against 64 bits: types of activations and
-tokens, odd widths and offsets, token counts on both sides of a chunk and a
-wave, tokens that all are the same, padded or out of range, and the parts of a
+tokens, odd widths and offsets, token counts on both sides of a chunk, a wave,
+a sorted run and of one and two merges of runs, tokens that all are the same, padded or out of range, and the parts of a
 row that are not the table's."""
 import pytest
 
@@ -11,7 +11,8 @@ pytestmark = pytest.mark.gpu
 # M, tokens, vocabulary, width, offset
 SHAPES = [(1, 1, 1, 1, 0), (3, 1, 5, 7, 1), (2, 31, 2, 8, 4), (1, 32, 3, 9, 2), (2, 33, 40, 512, 0), (1, 64, 511, 513, 3),
           (3, 65, 512, 64, 7), (1, 300, 513, 1, 0), (2, 1000, 37, 100, 5), (1, 1025, 70000, 17, 0), (2, 2500, 300, 1030, 9),
-          (1, 5000, 4, 520, 0), (5, 0, 10, 12, 2)]
+          (1, 5000, 4, 520, 0), (5, 0, 10, 12, 2), (1, 4096, 300, 3, 0), (2, 4097, 60, 9, 3), (1, 9000, 300001, 1, 2),
+          (1, 66000, 5, 3, 0), (2, 140001, 3000, 2, 1)]
 
 
 def _tokens(kind, M, N, V, dtype, gen):
