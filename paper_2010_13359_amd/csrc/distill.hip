@@ -119,17 +119,6 @@ __device__ float entry_gradient(const DistillArgs &a, const Message &s, int have
     return (exp_of<FINE>(a, s.z[j], x.largest) / x.total - sum) * coef;
 }
 
-// Keeps the compiler from holding a row's logits converted to 32 bits between
-// two passes over them, which takes twice the registers.
-template <typename V>
-__device__ __forceinline__ void forget(V &raw) {
-    typedef uint32_t Words __attribute__((ext_vector_type(sizeof(V) / 4)));
-    Words w = __builtin_bit_cast(Words, raw);
-#pragma unroll
-    for (unsigned i = 0; i < sizeof(V) / 4; ++i) asm("" : "+v"(w[i]));
-    raw = __builtin_bit_cast(V, w);
-}
-
 // NV vectors of 16 bytes per lane of a row's columns [0, V), and the last V % kPer
 // columns one each in the first lanes.  Vectors beyond the row are -inf.
 template <typename T, int W, int NV, bool STREAM>

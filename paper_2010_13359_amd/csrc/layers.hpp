@@ -78,6 +78,28 @@ struct Vec16 {
     typedef float wide __attribute__((ext_vector_type(16 / sizeof(T))));
 };
 
+// Keeps the compiler from holding a row converted to 32 bits between two passes
+// over it, which takes twice the registers.
+template <typename V>
+__device__ __forceinline__ void forget(V &raw) {
+    typedef uint32_t Words __attribute__((ext_vector_type(sizeof(V) / 4)));
+    Words w = __builtin_bit_cast(Words, raw);
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(V) / 4; ++i) asm("" : "+v"(w[i]));
+    raw = __builtin_bit_cast(V, w);
+}
+
+// The values are made here, and not where they are next used.
+template <typename V>
+__device__ __forceinline__ void settle(V &x) {
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(V) / 4; ++i) {
+        float f = x[i];
+        asm volatile("" : "+v"(f));
+        x[i] = f;
+    }
+}
+
 // An element's bits: a load that is not converted where it is issued.
 template <typename T>
 struct Bits {
@@ -96,9 +118,21 @@ __device__ __forceinline__ float widen_bits(typename Bits<T>::type b) {
     return static_cast<float>(__builtin_bit_cast(T, b));
 }
 
-template <typename T>
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ typename Vec16<T>::type load16(const T *p) {
-    return *reinterpret_cast<const typename Vec16<T>::packed *>(p);
+    const typename Vec16<T>::packed *v = reinterpret_cast<const typename Vec16<T>::packed *>(p);
+    return STREAM ? __builtin_nontemporal_load(v) : *v;
+}
+template <typename T, bool STREAM = false>
+__device__ __forceinline__ void store16(T *p, typename Vec16<T>::type v) {
+    if (STREAM)
+        __builtin_nontemporal_store(v, reinterpret_cast<typename Vec16<T>::packed *>(p));
+    else
+        *reinterpret_cast<typename Vec16<T>::packed *>(p) = v;
+}
+template <typename T>
+__device__ __forceinline__ typename Vec16<T>::type narrow(typename Vec16<T>::wide v) {
+    return __builtin_convertvector(v, typename Vec16<T>::type);
 }
 template <typename T>
 __device__ __forceinline__ typename Vec16<T>::wide widen(typename Vec16<T>::type v) {

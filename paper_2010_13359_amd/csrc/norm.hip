@@ -5,13 +5,42 @@
 namespace dq {
 namespace {
 
-// Row shapes: W waves per row, NV vectors of eight elements per lane, so that
-// a row of up to 512 W NV elements stays in registers between the statistics
-// and their use.
-template <int W>
-constexpr int kThreads = W < 4 ? 256 : 64 * W;
-template <int W>
-constexpr int kRowsPerGroup = W < 4 ? 4 / W : 1;
+// Row shapes: L lanes of a wave, or W whole waves, and NV vectors of 16 bytes per
+// lane, so that a row stays in registers between the statistics and their use.
+// The last D % kPer elements lie one each in the row's first lanes.
+template <int L, int W, int NV>
+struct Shape {
+    static constexpr int kLanes = W == 1 ? L : 64 * W, kThreads = W < 4 ? 256 : 64 * W, kRows = kThreads / kLanes;
+    // Backward: workgroups of all workers together, and the least rows of one where
+    // there are many, so that the partial sums are a fraction of what is read.  With
+    // 2048, 1024 and 512 workgroups rows of 64 bf16 elements (206 MB) take 55, 57 and
+    // 81 us, of 2048 (806 MB) 172, 173 and 188, of 4096 (806 MB) 175, 167 and 155.
+    static constexpr int kGroups = W == 1 ? 2048 : W * NV <= 4 ? 1024 : 512, kLeast = W == 1 ? 32 : 8;
+    static constexpr int kVectors = NV, kPerWave = W == 1 ? 64 / L : 1;  // rows a wave holds
+    // The first row of this wave's, in a scalar register: a loop over it keeps one
+    // set of sums.
+    static __device__ __forceinline__ int64_t first_row() {
+        return static_cast<int64_t>(blockIdx.x) * kRows +
+               (W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kPerWave : 0);
+    }
+    static __device__ __forceinline__ int row_of_wave() { return kPerWave == 1 ? 0 : (threadIdx.x & 63) / L; }
+    // sums over a row's lanes; `slot`: W floats of LDS per value
+    static __device__ __forceinline__ float sum(float x, float *slot) {
+        if (W > 1) return group_sum<W>(x, slot);
+        return L == 16 ? lanes_sum<16>(x) : wave_sum(x);
+    }
+    static __device__ __forceinline__ float2 sums(float x, float y, float *slot) {
+        if (W == 1) return make_float2(sum(x, slot), sum(y, slot));
+        x = wave_sum(x);
+        y = wave_sum(y);
+        if ((threadIdx.x & 63) == 0) {
+            slot[threadIdx.x >> 6] = x;
+            slot[W + (threadIdx.x >> 6)] = y;
+        }
+        __syncthreads();
+        return make_float2(lanes_sum<W>(slot[threadIdx.x & (W - 1)]), lanes_sum<W>(slot[W + (threadIdx.x & (W - 1))]));
+    }
+};
 
 struct NormArgs {
     const float *P;
@@ -21,57 +50,101 @@ struct NormArgs {
     float eps;
 };
 
-// Two passes over the registers: the mean, then the mean square of what is
-// left, so that a large mean costs the variance no digits.
-template <typename T, int W, int NV>
-__global__ __launch_bounds__(kThreads<W>) void k_norm_fwd(const T *x, NormArgs a, T *y, float *stats) {
-    __shared__ float slots[2][W];
-    const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t m = blockIdx.y, D = a.D;
-    f32x8 g[NV], b[NV];
+// Element i of a row whose start is the same in every lane: an address of a
+// scalar and a 32-bit part.
+template <typename T>
+__device__ __forceinline__ T *at(T *row, int i) {
+    return (T *)((const char *)row + static_cast<uint32_t>(i) * static_cast<uint32_t>(sizeof(T)));
+}
+
+// A lane's elements of a row, as they lie in memory; beyond the row its last ones
+// once more, so that loads need no branch.
+template <typename T, typename S, bool STREAM>
+struct Row {
+    typename Vec16<T>::type raw[S::kVectors];
+    typename Bits<T>::type last;
+    __device__ __forceinline__ void load(const T *p, int lane, int vectors, int rest) {
+        if (vectors > 0) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int64_t c = 8 * (lane + 64 * W * v);
-        g[v] = 1.0f;
-        b[v] = 0.0f;
-        if (a.gamma >= 0 && c < D) g[v] = load8(a.P + m * a.ldp + a.gamma + c, D - c);
-        if (a.beta >= 0 && c < D) b[v] = load8(a.P + m * a.ldp + a.beta + c, D - c);
-    }
-    const float inv = 1.0f / static_cast<float>(D);
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kRowsPerGroup<W>;
-    for (int64_t n = static_cast<int64_t>(blockIdx.x) * kRowsPerGroup<W> + (W == 1 ? threadIdx.x >> 6 : 0); n < a.N;
-         n += step) {
-        const T *row = x + (m * a.N + n) * D;
-        f32x8 f[NV];
-        float s = 0.0f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t c = 8 * (lane + 64 * W * v);
-            f[v] = load8(row + c, D - c);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s += f[v][i];
-        }
-        const float mean = group_sum<W>(s, slots[0]) * inv;
-        s = 0.0f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t c = 8 * (lane + 64 * W * v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                f[v][i] = c + i < D ? f[v][i] - mean : 0.0f;
-                s = fmaf(f[v][i], f[v][i], s);
+            for (int v = 0; v < S::kVectors; ++v) {
+                const int q = lane + S::kLanes * v;
+                raw[v] = load16<T, STREAM>(at(p, Vec16<T>::kPer * (q < vectors ? q : vectors - 1)));
             }
         }
-        const float rstd = 1.0f / sqrtf(group_sum<W>(s, slots[1]) * inv + a.eps);
+        if (rest > 0) last = load_bits(at(p, Vec16<T>::kPer * vectors + (lane < rest ? lane : 0)));
+    }
+};
+// ... and of a parameter's row.
+template <typename T, typename S>
+struct Params {
+    typename Vec16<T>::wide of[S::kVectors];
+    float last;
+    __device__ __forceinline__ void load(const float *p, float none, bool there, int lane, int vectors, int rest) {
+        last = none;
+#pragma unroll
+        for (int v = 0; v < S::kVectors; ++v) of[v] = none;
+        if (!there) return;
+#pragma unroll
+        for (int v = 0; v < S::kVectors; ++v)
+            if (lane + S::kLanes * v < vectors) of[v] = load_floats<T>(p + Vec16<T>::kPer * (lane + S::kLanes * v));
+        if (lane < rest) last = p[Vec16<T>::kPer * vectors + lane];
+    }
+};
+
+// Two passes over the registers: the mean, then the mean square of what is
+// left, so that a large mean costs the variance no digits.
+template <typename T, typename S, int STREAM>
+__global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a, T *y, float *stats) {
+    constexpr int kPer = Vec16<T>::kPer, NV = S::kVectors;
+    typedef typename Vec16<T>::wide Wide;
+    __shared__ float slots[2][16];
+    const int lane = threadIdx.x % S::kLanes;
+    const int64_t m = blockIdx.y, D = a.D;
+    const int vectors = static_cast<int>(D / kPer), rest = static_cast<int>(D % kPer);
+    Params<T, S> g, b;
+    g.load(a.P + m * a.ldp + a.gamma, 1.0f, a.gamma >= 0, lane, vectors, rest);
+    b.load(a.P + m * a.ldp + a.beta, 0.0f, a.beta >= 0, lane, vectors, rest);
+    const float inv = 1.0f / static_cast<float>(D);
+    const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
+    for (int64_t first = S::first_row(); first < a.N; first += step) {
+        const bool in = first + S::row_of_wave() < a.N;
+        const int64_t n = in ? first + S::row_of_wave() : a.N - 1;
+        Row<T, S, (STREAM > 1)> row;
+        row.load(x + (m * a.N + n) * D, lane, vectors, rest);
+        Wide f[NV];
+        float last = lane < rest ? widen_bits<T>(row.last) : 0.0f, s = last;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            f[v] = widen<T>(row.raw[v]);
+            float part = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) part += f[v][i];
+            s += lane + S::kLanes * v < vectors ? part : 0.0f;
+        }
+        const float mean = S::sum(s, slots[0]) * inv;
+        last -= mean;
+        s = lane < rest ? last * last : 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float part = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                f[v][i] -= mean;
+                part = fmaf(f[v][i], f[v][i], part);
+            }
+            s += lane + S::kLanes * v < vectors ? part : 0.0f;
+        }
+        const float rstd = 1.0f / sqrtf(S::sum(s, slots[1]) * inv + a.eps);
         T *out = y + (m * a.N + n) * D;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = 8 * (lane + 64 * W * v);
+            const int q = lane + S::kLanes * v;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[v][i] = fmaf(f[v][i] * rstd, g[v][i], b[v][i]);
-            store8(out + c, D - c, f[v]);
+            for (int i = 0; i < kPer; ++i) f[v][i] = fmaf(f[v][i] * rstd, g.of[v][i], b.of[v][i]);
+            if (q < vectors && in) store16<T, (STREAM > 0)>(at(out, kPer * q), narrow<T>(f[v]));
         }
-        if (stats && lane == 0) {
+        if (lane < rest && in) *at(out, kPer * vectors + lane) = static_cast<T>(fmaf(last * rstd, g.last, b.last));
+        if (stats && lane == 0 && in) {
             stats[2 * (m * a.N + n)] = mean;
             stats[2 * (m * a.N + n) + 1] = rstd;
         }
@@ -119,81 +192,109 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const T *x, NormArgs a, 
 // One workgroup takes every gridDim.x-th group of rows of its worker, keeps
 // its columns' sums of dy and dy * xh in registers meanwhile and leaves them in
 // part[m][blockIdx.x][2][D].
-template <typename T, int W, int NV>
-__global__ __launch_bounds__(kThreads<W>) void k_norm_bwd(const T *x, const T *dy, NormArgs a, const float *stats,
+template <typename T, typename S, int STREAM>
+__global__ __launch_bounds__(S::kThreads, S::kVectors < 3 || S::kThreads > 256 ? 4 : 2) void k_norm_bwd(const T *x, const T *dy, NormArgs a, const float *stats,
                                                           T *dx, float *part) {
-    __shared__ float slots[2][2][W];
-    const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    constexpr int kPer = Vec16<T>::kPer, NV = S::kVectors;
+    typedef typename Vec16<T>::wide Wide;
+    __shared__ float slots[2][2 * 16];
+    const int lane = threadIdx.x % S::kLanes;
     const int64_t m = blockIdx.y, D = a.D;
-    f32x8 g[NV], sg[NV], sb[NV];
+    const int vectors = static_cast<int>(D / kPer), rest = static_cast<int>(D % kPer);
+    Params<T, S> g;
+    g.load(a.P + m * a.ldp + a.gamma, 1.0f, a.gamma >= 0, lane, vectors, rest);
+    Wide sg[NV], sb[NV];
+    float last_sg = 0.0f, last_sb = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int64_t c = 8 * (lane + 64 * W * v);
-        g[v] = 1.0f;
-        if (a.gamma >= 0 && c < D) g[v] = load8(a.P + m * a.ldp + a.gamma + c, D - c);
         sg[v] = 0.0f;
         sb[v] = 0.0f;
     }
     const float inv = 1.0f / static_cast<float>(D);
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kRowsPerGroup<W>;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
     int turn = 0;
-    for (int64_t n = static_cast<int64_t>(blockIdx.x) * kRowsPerGroup<W> + (W == 1 ? threadIdx.x >> 6 : 0); n < a.N;
-         n += step, turn ^= 1) {
-        const int64_t at = (m * a.N + n) * D;
-        const float mean = stats[2 * (m * a.N + n)], rstd = stats[2 * (m * a.N + n) + 1];
-        f32x8 xh[NV], u[NV];
-        float s1 = 0.0f, s2 = 0.0f;
+    for (int64_t first = S::first_row(); first < a.N; first += step, turn ^= 1) {
+        const bool in = first + S::row_of_wave() < a.N;
+        const int64_t n = in ? first + S::row_of_wave() : a.N - 1;
+        const float2 st = reinterpret_cast<const float2 *>(stats)[m * a.N + n];
+        Row<T, S, (STREAM > 1)> rx, ry;
+        rx.load(x + (m * a.N + n) * D, lane, vectors, rest);
+        ry.load(dy + (m * a.N + n) * D, lane, vectors, rest);
+        const float mean = st.x, rstd = st.y;
+        const float last_xh = lane < rest ? (widen_bits<T>(rx.last) - mean) * rstd : 0.0f;
+        float last_u = lane < rest && in ? widen_bits<T>(ry.last) : 0.0f;
+        last_sg = fmaf(last_u, last_xh, last_sg);
+        last_sb += last_u;
+        last_u *= g.last;
+        float s1 = last_u, s2 = last_u * last_xh;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t c = 8 * (lane + 64 * W * v);
-            xh[v] = load8(x + at + c, D - c, mean);
-            u[v] = load8(dy + at + c, D - c);
+        for (int v = 0; v < NV; ++v) {  // sg and sb of lanes beyond the row are not stored
+            const Wide xv = widen<T>(rx.raw[v]);
+            Wide yv = widen<T>(ry.raw[v]);
+            if (S::kPerWave > 1 && !in) yv = 0.0f;
+            float p1 = 0.0f, p2 = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                xh[v][i] = (xh[v][i] - mean) * rstd;
-                sg[v][i] = fmaf(u[v][i], xh[v][i], sg[v][i]);
-                sb[v][i] += u[v][i];
-                u[v][i] *= g[v][i];
-                s1 += u[v][i];
-                s2 = fmaf(u[v][i], xh[v][i], s2);
+            for (int i = 0; i < kPer; ++i) {
+                const float xh = (xv[i] - mean) * rstd, u = yv[i] * g.of[v][i];
+                sg[v][i] = fmaf(yv[i], xh, sg[v][i]);
+                sb[v][i] += yv[i];
+                p1 += u;
+                p2 = fmaf(u, xh, p2);
             }
+            s1 += lane + S::kLanes * v < vectors ? p1 : 0.0f;
+            s2 += lane + S::kLanes * v < vectors ? p2 : 0.0f;
+            settle(sg[v]);  // one vector's temporaries at a time
+            settle(sb[v]);
+            asm volatile("" : "+v"(s1), "+v"(s2));
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (!dx) continue;
-        const float c1 = group_sum<W>(s1, slots[turn][0]) * inv, c2 = group_sum<W>(s2, slots[turn][1]) * inv;
+        if (dx) {
+            const float2 c = S::sums(s1, s2, slots[turn]);
+            const float c1 = c.x * inv, c2 = c.y * inv;
+            T *out = dx + (m * a.N + n) * D;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t c = 8 * (lane + 64 * W * v);
+            for (int v = 0; v < NV; ++v) {
+                const int q = lane + S::kLanes * v;
+                forget(rx.raw[v]);
+                forget(ry.raw[v]);
+                const Wide xv = widen<T>(rx.raw[v]), yv = widen<T>(ry.raw[v]);
+                Wide d;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[v][i] = rstd * (u[v][i] - c1 - xh[v][i] * c2);
-            store8(dx + at + c, D - c, u[v]);
+                for (int i = 0; i < kPer; ++i) d[i] = rstd * (yv[i] * g.of[v][i] - c1 - (xv[i] - mean) * rstd * c2);
+                if (q < vectors && in) store16<T, (STREAM > 0)>(at(out, kPer * q), narrow<T>(d));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (lane < rest && in) *at(out, kPer * vectors + lane) = static_cast<T>(rstd * (last_u - c1 - last_xh * c2));
         }
     }
     if (!part) return;
-    constexpr int R = kRowsPerGroup<W>;
-    __shared__ float sums[R > 1 ? R - 1 : 1][R > 1 ? 64 : 1][8];
+    // the workgroup's rows hold the same columns; summed in their order
+    constexpr int R = S::kRows, kWidth = S::kLanes * NV * kPer;
+    __shared__ float sums[R > 1 ? R : 1][R > 1 ? kWidth : 1], tails[R > 1 ? R : 1][R > 1 ? S::kLanes : 1];
     float *to = part + (m * gridDim.x + blockIdx.x) * 2 * D;
+    for (int k = 0; k < 2; ++k, to += D) {
+        if (R == 1) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+            for (int v = 0; v < NV; ++v)
+                if (lane + S::kLanes * v < vectors)
+                    store_floats<T>(to + kPer * (lane + S::kLanes * v), k == 0 ? sg[v] : sb[v]);
+            if (lane < rest) to[kPer * vectors + lane] = k == 0 ? last_sg : last_sb;
+            continue;
+        }
+        const int r = threadIdx.x / S::kLanes;
+        __syncthreads();
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t c = 8 * (lane + 64 * W * v);
-            f32x8 s = k == 0 ? sg[v] : sb[v];
-            if (R > 1) {  // the group's waves hold the same columns
-                const int w = threadIdx.x >> 6;
-                __syncthreads();
-                if (w > 0) {
+        for (int v = 0; v < NV; ++v)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sums[w - 1][lane][i] = s[i];
-                }
-                __syncthreads();
-                if (w == 0) {
+            for (int i = 0; i < kPer; ++i) sums[r][kPer * (lane + S::kLanes * v) + i] = k == 0 ? sg[v][i] : sb[v][i];
+        tails[r][lane] = k == 0 ? last_sg : last_sb;
+        __syncthreads();
+        for (int c = threadIdx.x; c < D; c += S::kThreads) {
+            const bool tail = c >= kPer * vectors;
+            float s = 0.0f;
 #pragma unroll
-                    for (int r = 0; r < R - 1; ++r)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) s[i] += sums[r][lane][i];
-                }
-            }
-            if (R == 1 || threadIdx.x < 64) store8(to + k * D + c, D - c, s);
+            for (int q = 0; q < R; ++q) s += tail ? tails[q][c - kPer * vectors] : sums[q][c];
+            to[c] = s;
         }
     }
 }
@@ -253,22 +354,28 @@ __global__ __launch_bounds__(256) void k_norm_sums_long(const T *x, const T *dy,
     store8(to + D, D - c, sb);
 }
 
-// G's weight and bias from the shares' sums: 64 columns per workgroup, four
-// quarters of the shares side by side.
-__global__ __launch_bounds__(256) void k_norm_params(const float *part, int shares, NormArgs a, int64_t ld, float *G,
-                                                     bool add) {
-    __shared__ float quarter[3][64];
-    const int64_t m = blockIdx.y, D = a.D, col = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63);
-    const int q = threadIdx.x >> 6;
+// G's weight and bias from the shares' sums: 64 columns per workgroup, its waves
+// taking every 16th share, eight of them on their way at a time.
+__global__ __launch_bounds__(1024) void k_norm_params(const float *part, int shares, NormArgs a, int64_t ld, float *G,
+                                                      bool add) {
+    constexpr int kWaves = 16, kBatch = 8;
+    __shared__ float sums[kWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t m = blockIdx.y, D = a.D, col = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+    const float *p = part + m * shares * 2 * D + (col < 2 * D ? col : 2 * D - 1);
     float s = 0.0f;
-    if (col < 2 * D) {
-        const float *p = part + m * shares * 2 * D + col;
-        for (int b = q; b < shares; b += 4) s += p[static_cast<int64_t>(b) * 2 * D];
+    for (int b = wave; b < shares; b += kWaves * kBatch) {
+        float f[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) f[u] = p[static_cast<int64_t>(b + kWaves * u < shares ? b + kWaves * u : b) * 2 * D];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (b + kWaves * u < shares) s += f[u];
     }
-    if (q > 0) quarter[q - 1][threadIdx.x & 63] = s;
+    sums[wave][lane] = s;
     __syncthreads();
-    if (q > 0 || col >= 2 * D) return;
-    s = ((s + quarter[0][threadIdx.x]) + quarter[1][threadIdx.x]) + quarter[2][threadIdx.x];
+    if (wave > 0 || col >= 2 * D) return;
+    for (int w = 1; w < kWaves; ++w) s += sums[w][lane];
     const int64_t base = col < D ? a.gamma : a.beta;
     if (base < 0) return;
     float *to = G + m * ld + base + (col < D ? col : col - D);
@@ -277,21 +384,35 @@ __global__ __launch_bounds__(256) void k_norm_params(const float *part, int shar
 
 // ---------------------------------------------------------------------------
 
-constexpr int64_t kGroups = 2048;    // workgroups that fill the card several times over
-constexpr int64_t kWidest = 32768;   // 16 waves, four vectors a lane
+constexpr int kForwardMost = 32768, kBackwardMost = 16384;  // widest rows that stay in registers
 
-// Workgroups per worker of the kernels that loop over rows.
-int64_t forward_groups(int64_t M, int64_t N, int rows_per_group) {
-    const int64_t most = ceil_div(N, rows_per_group), want = ceil_div(kGroups, M);
+// Workgroups per worker of the forward pass: 8192 in all, and 2048 of wide rows,
+// whose weight and bias are as much to read as a row (8192 and 2048: rows of 2048
+// bf16 elements, 537 MB, 95.6 and 103 us, of 16384 127 and 106).
+int64_t forward_groups(int64_t M, int64_t N, int rows_per_group, int threads) {
+    const int64_t most = ceil_div(N, rows_per_group), want = ceil_div(threads > 256 ? 2048 : 8192, M);
     return most < want ? most : want;
 }
-// Shares of the rows whose columns' sums are kept apart: enough to fill the
-// card, and at least 16 rows each, so that their partial sums are a fraction
-// of what is read.
-int backward_shares(int64_t M, int64_t N) {
-    const int64_t want = ceil_div(1024, M), most = ceil_div(N, 16);
+int shares_of(int64_t M, int64_t N, int groups, int least) {
+    const int64_t want = ceil_div(groups, M), most = ceil_div(N, M * N < 8192 ? 8 : least);
     const int64_t s = most < want ? most : want;
     return static_cast<int>(s < 1 ? 1 : s);
+}
+
+// How the rows pass by the caches, by the bytes of all of them: 0 not, 1 what is
+// written, 2 what is read too.  Forward, 8192 rows of 2048 bf16 for each of 8
+// workers (537 MB): 95.6 us written so, 107.5 not; 66 MB the same.  Backward, f32,
+// 1611 MB: 307 us not, 299 written so, 274 both; bf16, 98 MB: 25.4, 22.3 and 24.9.
+int forward_streams(double bytes) { return bytes > 100e6 ? 1 : 0; }
+int backward_streams(double bytes) { return bytes > 200e6 ? 2 : bytes > 80e6 ? 1 : 0; }
+template <typename F>
+void with_streams(int streams, F &&f) {
+    if (streams == 0)
+        f(std::integral_constant<int, 0>{});
+    else if (streams == 1)
+        f(std::integral_constant<int, 1>{});
+    else
+        f(std::integral_constant<int, 2>{});
 }
 
 dqgan_status check(dqgan_plan P, const dqgan_norm_desc *d, int64_t ldp) {
@@ -311,24 +432,48 @@ NormArgs args(const dqgan_norm_desc *d, const float *P, int64_t ldp) {
     return NormArgs{P, ldp, d->gamma, d->beta, d->width, d->tokens, d->eps};
 }
 
-// f(W, NV) with the smallest row shape that holds D.
-template <typename F>
-void with_shape(int64_t D, F &&f) {
-    using std::integral_constant;
-    if (D <= 512)
-        f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-    else if (D <= 1024)
-        f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
-    else if (D <= 2048)
-        f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    else if (D <= 4096)
-        f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-    else if (D <= 8192)
-        f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    else if (D <= 16384)
-        f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
-    else
-        f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+// f(Shape{}) with the smallest row shape that holds D elements of T; returns
+// false, f not called, if D is above MOST.  16 waves of four vectors have 128
+// registers a lane, too few for the backward pass of 16-bit types.
+template <typename T, int MOST, typename F>
+bool with_shape(int64_t D, F &&f) {
+    const int64_t vectors = D / Vec16<T>::kPer;
+    if (vectors <= 16)
+        f(Shape<16, 1, 1>{});
+    else if (vectors <= 32)
+        f(Shape<16, 1, 2>{});
+    else if (vectors <= 64)
+        f(Shape<64, 1, 1>{});
+    else if (vectors <= 128)
+        f(Shape<64, 1, 2>{});
+    else if (vectors <= 256)
+        f(Shape<64, 4, 1>{});
+    else if (vectors <= 512)
+        f(Shape<64, 4, 2>{});
+    else if (vectors <= 768)
+        f(Shape<64, 4, 3>{});
+    else if (vectors <= 1024)
+        f(Shape<64, 4, 4>{});
+    else if (vectors <= 2048)
+        f(Shape<64, 16, 2>{});
+    else if constexpr (MOST / Vec16<T>::kPer > 2048) {
+        if (vectors > 4096 || D > MOST) return false;
+        f(Shape<64, 16, 4>{});
+    } else
+        return false;
+    return true;
+}
+
+// Shares of a worker's rows whose columns' sums are kept apart.
+int backward_shares(int64_t M, const dqgan_norm_desc *d) {
+    int shares = shares_of(M, d->tokens, 512, 8);
+    with_type(d->type, [&](auto t) {
+        with_shape<decltype(t), kBackwardMost>(d->width, [&](auto s) {
+            using S = decltype(s);
+            shares = shares_of(M, d->tokens, S::kGroups, S::kLeast);
+        });
+    });
+    return shares;
 }
 
 }  // namespace
@@ -353,17 +498,19 @@ dqgan_status dqgan_norm_forward(dqgan_plan P, const dqgan_norm_desc *d, const vo
     const int64_t M = P->desc.M;
     with_type(d->type, [&](auto t) {
         using T = decltype(t);
-        if (d->width > kWidest) {
-            const dim3 grid(static_cast<uint32_t>(forward_groups(M, d->tokens, 1)), static_cast<uint32_t>(M));
-            k_norm_fwd_long<T><<<grid, 1024, 0, st>>>(static_cast<const T *>(x), a, static_cast<T *>(y), stats);
-            return;
-        }
-        with_shape(d->width, [&](auto w, auto nv) {
-            constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-            const dim3 grid(static_cast<uint32_t>(forward_groups(M, d->tokens, kRowsPerGroup<W>)),
-                            static_cast<uint32_t>(M));
-            k_norm_fwd<T, W, NV><<<grid, kThreads<W>, 0, st>>>(static_cast<const T *>(x), a, static_cast<T *>(y), stats);
-        });
+        const T *from = static_cast<const T *>(x);
+        T *to = static_cast<T *>(y);
+        const uint32_t my = static_cast<uint32_t>(M);
+        if (!with_shape<T, kForwardMost>(d->width, [&](auto s) {
+                using S = decltype(s);
+                const dim3 grid(static_cast<uint32_t>(forward_groups(M, d->tokens, S::kRows, S::kThreads)), my);
+                if (forward_streams(2.0 * sizeof(T) * M * d->tokens * d->width))
+                    k_norm_fwd<T, S, 1><<<grid, S::kThreads, 0, st>>>(from, a, to, stats);
+                else
+                    k_norm_fwd<T, S, 0><<<grid, S::kThreads, 0, st>>>(from, a, to, stats);
+            }))
+            k_norm_fwd_long<T><<<dim3(static_cast<uint32_t>(forward_groups(M, d->tokens, 1, 1024)), my), 1024, 0, st>>>(
+                from, a, to, stats);
     });
     return launched();
 }
@@ -372,7 +519,7 @@ dqgan_status dqgan_norm_bytes(dqgan_plan P, const dqgan_norm_desc *d, size_t *by
     DQ_TRY(check(P, d, 0));
     if (!bytes) return DQGAN_EINVAL;
     const bool sums = d->tokens > 0 && (d->gamma >= 0 || d->beta >= 0);
-    *bytes = sums ? sizeof(float) * 2 * static_cast<size_t>(d->width) * P->desc.M * backward_shares(P->desc.M, d->tokens)
+    *bytes = sums ? sizeof(float) * 2 * static_cast<size_t>(d->width) * P->desc.M * backward_shares(P->desc.M, d)
                   : 0;
     return DQGAN_OK;
 }
@@ -393,35 +540,33 @@ dqgan_status dqgan_norm_backward(dqgan_plan P, const dqgan_norm_desc *d, const v
     hipStream_t st = static_cast<hipStream_t>(stream);
     NormArgs a = args(d, params, ldp);
     const int64_t M = P->desc.M, D = d->width;
-    const int shares = any ? backward_shares(M, d->tokens) : 0;
+    const int shares = any ? backward_shares(M, d) : 0;
     float *part = sums ? static_cast<float *>(workspace) : nullptr;
     if (any && (dx || sums)) {
         with_type(d->type, [&](auto t) {
             using T = decltype(t);
             const T *xt = static_cast<const T *>(x), *dyt = static_cast<const T *>(dy);
             T *dxt = static_cast<T *>(dx);
-            if (D > kWidest) {
-                if (sums) {  // first: dx may be dy
-                    const dim3 grid(static_cast<uint32_t>(ceil_div(D, 2048)), static_cast<uint32_t>(shares),
-                                    static_cast<uint32_t>(M));
-                    k_norm_sums_long<T><<<grid, 256, 0, st>>>(xt, dyt, a, stats, shares, part);
-                }
-                if (dx) {
-                    const dim3 grid(static_cast<uint32_t>(forward_groups(M, d->tokens, 1)), static_cast<uint32_t>(M));
-                    k_norm_bwd_long<T><<<grid, 1024, 0, st>>>(xt, dyt, a, stats, dxt);
-                }
+            const uint32_t my = static_cast<uint32_t>(M), of = static_cast<uint32_t>(shares);
+            if (with_shape<T, kBackwardMost>(D, [&](auto s) {
+                    using S = decltype(s);
+                    with_streams(backward_streams(3.0 * sizeof(T) * M * d->tokens * D), [&](auto streams) {
+                        k_norm_bwd<T, S, decltype(streams)::value><<<dim3(of, my), S::kThreads, 0, st>>>(
+                            xt, dyt, a, stats, dxt, part);
+                    });
+                }))
                 return;
-            }
-            with_shape(D, [&](auto w, auto nv) {
-                constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-                const dim3 grid(static_cast<uint32_t>(shares), static_cast<uint32_t>(M));
-                k_norm_bwd<T, W, NV><<<grid, kThreads<W>, 0, st>>>(xt, dyt, a, stats, dxt, part);
-            });
+            if (sums)  // first: dx may be dy
+                k_norm_sums_long<T><<<dim3(static_cast<uint32_t>(ceil_div(D, 2048)), of, my), 256, 0, st>>>(
+                    xt, dyt, a, stats, shares, part);
+            if (dx)
+                k_norm_bwd_long<T><<<dim3(static_cast<uint32_t>(forward_groups(M, d->tokens, 1, 1024)), my), 1024, 0, st>>>(
+                    xt, dyt, a, stats, dxt);
         });
     }
     if (sums && (any || !add)) {
         const dim3 grid(static_cast<uint32_t>(ceil_div(2 * D, 64)), static_cast<uint32_t>(M));
-        k_norm_params<<<grid, 256, 0, st>>>(part, shares, a, P->desc.ld, G, add != 0);
+        k_norm_params<<<grid, 1024, 0, st>>>(part, shares, a, P->desc.ld, G, add != 0);
     }
     return launched();
 }
