@@ -30,26 +30,55 @@ struct EmbedArgs {
     float scale;
 };
 
-// `lanes` (a power of two) consecutive threads per token.
-template <typename T, typename I>
+// 1 << shift consecutive threads per token, four channels each, forward_rows
+// tokens at a time: their rows are asked for before the first is used (one at a
+// time: 74.6 us where four take 47.3).  A padded place reads
+// the table's first row and writes 0.
+template <typename T>
+constexpr int forward_rows = sizeof(T) == 4 ? 2 : 4;
+template <typename T, typename I, bool STREAM>
 __global__ __launch_bounds__(256) void k_embed_fwd(const I *tok, const float *P, int64_t ldp, EmbedArgs a, int shift,
                                                    T *out) {
-    const int64_t m = blockIdx.y;
+    constexpr int kRows = forward_rows<T>;
+    typedef T Four __attribute__((ext_vector_type(4)));
+    typedef T FourAnywhere __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    const int64_t m = blockIdx.y, vectors = a.D >> 2;
     const int lanes = 1 << shift, per = 256 >> shift, lane = threadIdx.x & (lanes - 1);
-    for (int64_t n = static_cast<int64_t>(blockIdx.x) * per + (threadIdx.x >> shift); n < a.N;
-         n += static_cast<int64_t>(gridDim.x) * per) {
-        const I t = tok[m * a.N + n];
-        const bool there = t >= 0 && static_cast<int64_t>(t) < a.V;
-        const float *row = P + m * ldp + a.offset + (there ? static_cast<int64_t>(t) : 0) * a.D;
-        T *to = out + (m * a.N + n) * a.D;
-        for (int64_t c = 8 * lane; c < a.D; c += 8 * lanes) {
-            f32x8 f = 0.0f;
-            if (there) {
-                f = load8(row + c, a.D - c);
+    const float *table = P + m * ldp + a.offset;
+    tok += m * a.N;
+    out += m * a.N * a.D;
+    for (int64_t n = (static_cast<int64_t>(blockIdx.x) * per * kRows) + (threadIdx.x >> shift); n < a.N;
+         n += static_cast<int64_t>(gridDim.x) * per * kRows) {
+        const float *row[kRows];
+        bool there[kRows];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= a.scale;
+        for (int u = 0; u < kRows; ++u) {
+            const int64_t i = n + u * per < a.N ? n + u * per : n;
+            const I t = tok[i];
+            there[u] = t >= 0 && static_cast<int64_t>(t) < a.V;
+            row[u] = table + (there[u] ? static_cast<int64_t>(t) : 0) * a.D;
+        }
+        for (int64_t q = lane; q < vectors; q += lanes) {
+            f32x4 f[kRows];
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) f[u] = load_floats<float>(row[u] + 4 * q);
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                if (n + u * per >= a.N) break;
+                f[u] = there[u] ? f[u] * a.scale : f32x4(0.0f);
+                FourAnywhere *to = reinterpret_cast<FourAnywhere *>(out + (n + u * per) * a.D + 4 * q);
+                const Four v = __builtin_convertvector(f[u], Four);
+                if (STREAM)
+                    __builtin_nontemporal_store(v, to);
+                else
+                    *to = v;
             }
-            store8(to + c, a.D - c, f);
+        }
+        const int64_t c = 4 * vectors + lane;
+        if (lane < 4 && c < a.D) {
+            for (int u = 0; u < kRows; ++u)
+                if (n + u * per < a.N)
+                    out[(n + u * per) * a.D + c] = static_cast<T>(there[u] ? row[u][c] * a.scale : 0.0f);
         }
     }
 }
@@ -263,7 +292,7 @@ struct Channels {
 };
 
 constexpr int kBatch = 8;
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void k_embed_sum(const uint32_t *key, const uint32_t *at, const T *dout, EmbedArgs a,
                                                    int64_t chunks, int slabs, int width, float *part, float *G, bool add) {
     static_assert(2 * kChunk <= 64, "a lane for each place of a chunk and the next");
@@ -315,7 +344,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const uint32_t *key, const ui
         }
         if (ch.some_whole) {
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) raw[u] = load16(row[u] + ch.from);
+            for (int u = 0; u < kBatch; ++u) raw[u] = load16<T, STREAM>(row[u] + ch.from);
         }
         if (ch.some_tail) {
 #pragma unroll
@@ -464,6 +493,13 @@ void with_index(int32_t type, F &&f) {
         f(int64_t{});
 }
 
+// Whether `out` passes by the caches: 134 MB 47.3 us so and 52.8 not, 33 MB 13.4
+// and 15.7 (rows of 501 bf16: 15.1 and 14.1), 17 MB the same.
+bool forward_streams(double bytes) { return bytes > 30e6; }
+// Whether dout passes by the caches: 268 MB 148 us (the whole gradient) so and 181
+// not, 134 MB 356 and 365, 33 MB 118 and 114.
+bool backward_streams(double bytes) { return bytes > 100e6; }
+
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
 // The workspace: lists of tokens and of their places (two pairs where runs are
@@ -490,16 +526,20 @@ dqgan_status dqgan_embed_forward(dqgan_plan P, const dqgan_embed_desc *d, const 
     if (!any) return DQGAN_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const EmbedArgs a = args(P, d);
-    int shift = 0;
-    while (shift < 8 && (int64_t(8) << shift) < a.D) ++shift;
-    const int64_t groups = ceil_div(a.N, 256 >> shift);
-    const dim3 grid(static_cast<uint32_t>(groups < 65536 ? groups : 65536), static_cast<uint32_t>(P->desc.M));
+    int shift = 2;  // at least the four lanes of the last D % 4 channels
+    while (shift < 8 && (int64_t(4) << shift) < a.D) ++shift;
     with_type(d->type, [&](auto t) {
         with_index(d->index_type, [&](auto i) {
             using T = decltype(t);
             using I = decltype(i);
-            k_embed_fwd<T, I><<<grid, 256, 0, st>>>(static_cast<const I *>(tok), params, ldp, a, shift,
-                                                    static_cast<T *>(out));
+            const int64_t groups = ceil_div(a.N, forward_rows<T> * (256 >> shift));
+            const dim3 grid(static_cast<uint32_t>(groups < 65536 ? groups : 65536), static_cast<uint32_t>(P->desc.M));
+            if (forward_streams(static_cast<double>(sizeof(T)) * P->desc.M * a.N * a.D))
+                k_embed_fwd<T, I, true><<<grid, 256, 0, st>>>(static_cast<const I *>(tok), params, ldp, a, shift,
+                                                              static_cast<T *>(out));
+            else
+                k_embed_fwd<T, I, false><<<grid, 256, 0, st>>>(static_cast<const I *>(tok), params, ldp, a, shift,
+                                                               static_cast<T *>(out));
         });
     });
     return launched();
@@ -559,8 +599,11 @@ dqgan_status dqgan_embed_backward(dqgan_plan P, const dqgan_embed_desc *d, const
         using T = decltype(t);
         const int slabs = slabs_of(a.D, Vec16<T>::kPer), width = width_of(a.D, Vec16<T>::kPer);
         const uint32_t my = static_cast<uint32_t>(M);
-        k_embed_sum<T><<<dim3(static_cast<uint32_t>(ceil_div(chunks * slabs, 4)), my), 256, 0, st>>>(
-            key[now], at[now], static_cast<const T *>(dout), a, chunks, slabs, width, part, G, add != 0);
+        with_stream(backward_streams(static_cast<double>(sizeof(T)) * M * a.N * a.D), [&](auto streams) {
+            k_embed_sum<T, decltype(streams)::value>
+                <<<dim3(static_cast<uint32_t>(ceil_div(chunks * slabs, 4)), my), 256, 0, st>>>(
+                    key[now], at[now], static_cast<const T *>(dout), a, chunks, slabs, width, part, G, add != 0);
+        });
         if (chunks > 2)
             k_embed_join<T><<<dim3(static_cast<uint32_t>(ceil_div(chunks, kJoinChunks) * slabs), my), 64 * kJoinWaves, 0, st>>>(
                 key[now], a, chunks, slabs, width, part, G, add != 0);
