@@ -1,7 +1,11 @@
 // Embedding lookup of M workers, each from its own table in its row of P, and
 // its gradient, summed over sorted tokens into the worker's row of G.
 //
-// The gradient's launches:
+// The gradient of up to kFew tokens is one launch, k_embed_few: a workgroup owns
+// some rows of the table, writes 0 to them and then the sums of those that are
+// tokens; each wave has all tokens in its lanes.
+//
+// The launches of more:
 //   k_embed_sort   sorts runs of kRun tokens, one workgroup each (stable, so that
 //                  equal ones stay in their order); the other workgroups of the
 //                  launch write the table's part of G as 0 meanwhile;
@@ -81,6 +85,17 @@ __global__ __launch_bounds__(256) void k_embed_fwd(const I *tok, const float *P,
                     out[(n + u * per) * a.D + c] = static_cast<T>(there[u] ? row[u][c] * a.scale : 0.0f);
         }
     }
+}
+
+// Zeros to n floats from `to` on, in vectors from a 16-byte boundary on; thread
+// `tid` of `threads`.
+__device__ __forceinline__ void fill(float *to, int64_t n, int64_t tid, int64_t threads) {
+    const int64_t ahead = (16 - (reinterpret_cast<uintptr_t>(to) & 15)) / 4 & 3, head = ahead < n ? ahead : n;
+    const int64_t quads = (n - head) / 4;
+    f32x4 *v = reinterpret_cast<f32x4 *>(to + head);
+    for (int64_t q = tid; q < quads; q += threads) v[q] = 0.0f;
+    if (tid < head) to[tid] = 0.0f;
+    if (tid < n - head - 4 * quads) to[head + 4 * quads + tid] = 0.0f;
 }
 
 // A worker's tokens to sort: padded places count as token V, behind all others.
@@ -176,18 +191,11 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const I *tok, Embed
                  at + first);
         return;
     }
-    // the table's part of G, from a 16-byte boundary on in vectors
-    const int64_t b = blockIdx.x - sorts, m = b / fills, len = a.V * a.D;
-    float *to = G + m * a.ld + a.offset;
-    const int64_t head = len < ((4 - (a.offset & 3)) & 3) ? len : ((4 - (a.offset & 3)) & 3);
-    const int64_t quads = (len - head) / 4, each = (quads + fills - 1) / fills;
-    const int64_t first = (b % fills) * each, last = first + each < quads ? first + each : quads;
-    f32x4 *v = reinterpret_cast<f32x4 *>(to + head);
-    for (int64_t q = first + threadIdx.x; q < last; q += kSortThreads) v[q] = 0.0f;
-    if (b % fills == 0) {
-        if (threadIdx.x < head) to[threadIdx.x] = 0.0f;
-        if (threadIdx.x < ((len - head) & 3)) to[head + 4 * quads + threadIdx.x] = 0.0f;
-    }
+    // an equal part of a table's part of G, in whole quads
+    const int64_t b = blockIdx.x - sorts, m = b / fills, len = a.V * a.D, each = ((len + fills - 1) / fills + 3) & ~int64_t(3);
+    const int64_t first = (b % fills) * each;
+    if (first < len)
+        fill(G + m * a.ld + a.offset + first, len - first < each ? len - first : each, threadIdx.x, kSortThreads);
 }
 
 // Runs of `len` places (at least a workgroup's 256) to runs of kFan * len: a
@@ -292,6 +300,88 @@ struct Channels {
 };
 
 constexpr int kBatch = 8;
+// Against the launches of more, 128 tokens for each of M workers' tables of V x D
+// (bf16): 1 x 1000 x 1024 8.4 and 22.4 us, 1 x 32000 x 1024 25.4 and 41.7, 8 x 150 x 64
+// 11.3 and 19.0, 16 x 30000 x 64 34.9 and 40.7; 256 tokens 8.3 and 22.8, 28.0 and
+// 41.7, 16.6 and 19.8, 47.0 and 41.2, as a row's tokens are added one after the other.
+constexpr int kFewRounds = 3, kFew = 64 * kFewRounds, kFewWaves = 8, kFewBatch = 4;
+template <typename T, typename I>
+__global__ __launch_bounds__(64 * kFewWaves) void k_embed_few(const I *tok, const T *dout, EmbedArgs a, int64_t rows,
+                                                              int slabs, int width, float *G, bool add) {
+    const int64_t m = blockIdx.y, row0 = static_cast<int64_t>(blockIdx.x) * rows;
+    const int64_t mine = a.V - row0 < rows ? a.V - row0 : rows;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    dout += m * a.N * a.D;
+    G += m * a.ld + a.offset + row0 * a.D;
+    uint32_t row[kFewRounds];
+    uint64_t todo[kFewRounds], any = 0;
+#pragma unroll
+    for (int j = 0; j < kFewRounds; ++j) {
+        const int i = 64 * j + lane;
+        const int64_t t = i < a.N ? static_cast<int64_t>(tok[m * a.N + i]) : -1;
+        const bool hit = t >= row0 && t < row0 + mine;
+        row[j] = hit ? static_cast<uint32_t>(t - row0) : UINT32_MAX;
+        todo[j] = __ballot(hit);
+        any |= todo[j];
+    }
+    if (!add) fill(G, mine * a.D, tid, 64 * kFewWaves);
+    if (any == 0) return;
+    __syncthreads();  // the zeros come before the sums
+    int task = 0;
+#pragma unroll
+    for (int j = 0; j < kFewRounds; ++j) {
+        while (todo[j] != 0) {
+            const uint32_t r = __builtin_amdgcn_readlane(row[j], __ffsll(static_cast<long long>(todo[j])) - 1);
+            uint64_t of_row[kFewRounds];
+#pragma unroll
+            for (int i = 0; i < kFewRounds; ++i) {
+                of_row[i] = i < j ? 0 : __ballot(row[i] == r);
+                todo[i] &= ~of_row[i];
+            }
+            for (int slab = 0; slab < slabs; ++slab, ++task) {
+                if (task % kFewWaves != wave) continue;
+                const Channels<T> ch(a.D, slab, slabs, width, lane);
+                typename Vec16<T>::wide s = 0.0f;
+                float last_s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kFewRounds; ++i) {
+                    for (uint64_t same = of_row[i]; same != 0;) {
+                        const T *from[kFewBatch];
+                        int count = 0;
+#pragma unroll
+                        for (int u = 0; u < kFewBatch; ++u) {
+                            if (same != 0) {
+                                from[u] = dout + (64 * i + __ffsll(static_cast<long long>(same)) - 1) * a.D;
+                                same &= same - 1;
+                                ++count;
+                            } else {
+                                from[u] = from[0];
+                            }
+                        }
+                        typename Vec16<T>::type raw[kFewBatch];
+                        typename Bits<T>::type last[kFewBatch];
+                        if (ch.some_whole) {
+#pragma unroll
+                            for (int u = 0; u < kFewBatch; ++u) raw[u] = load16(from[u] + ch.from);
+                        }
+                        if (ch.some_tail) {
+#pragma unroll
+                            for (int u = 0; u < kFewBatch; ++u) last[u] = load_bits(from[u] + ch.from_tail);
+                        }
+#pragma unroll
+                        for (int u = 0; u < kFewBatch; ++u) {
+                            if (u >= count) break;
+                            if (ch.some_whole) s += widen<T>(raw[u]);
+                            if (ch.some_tail) last_s += widen_bits<T>(last[u]);
+                        }
+                    }
+                }
+                ch.put(G + static_cast<int64_t>(r) * a.D, s, last_s, a.scale, add);
+            }
+        }
+    }
+}
+
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void k_embed_sum(const uint32_t *key, const uint32_t *at, const T *dout, EmbedArgs a,
                                                    int64_t chunks, int slabs, int width, float *part, float *G, bool add) {
@@ -470,6 +560,15 @@ int slabs_of(int64_t D, int per) {
 }
 int width_of(int64_t D, int per) { return static_cast<int>(ceil_div(D / per, slabs_of(D, per))); }
 
+// Rows of a workgroup of k_embed_few: 8 to 128 KB of G, to fill the card.
+int64_t few_rows(int64_t M, int64_t V, int64_t D) {
+    int64_t floats = M * V * D / 4096;
+    if (floats < 2048) floats = 2048;
+    if (floats > kFillFloats) floats = kFillFloats;
+    const int64_t rows = floats / D;
+    return rows < 1 ? 1 : rows;
+}
+
 dqgan_status check(dqgan_plan P, const dqgan_embed_desc *d) {
     if (!P || !d) return DQGAN_EINVAL;
     const int64_t n = P->desc.d;
@@ -549,7 +648,7 @@ dqgan_status dqgan_embed_bytes(dqgan_plan P, const dqgan_embed_desc *d, size_t *
     DQ_TRY(check(P, d));
     if (!bytes) return DQGAN_EINVAL;
     const int64_t M = P->desc.M;
-    *bytes = d->tokens == 0 ? 0
+    *bytes = d->tokens <= kFew ? 0
                             : 2 * pairs_of(d->tokens) * list_bytes(M, d->tokens) +
                                   sizeof(float) * 2 * static_cast<size_t>(M * chunks_of(d->tokens)) * d->width;
     return DQGAN_OK;
@@ -562,11 +661,25 @@ dqgan_status dqgan_embed_backward(dqgan_plan P, const dqgan_embed_desc *d, const
     DQ_TRY(check_ptr(tok, any));
     DQ_TRY(check_ptr(dout, any));
     DQ_TRY(check_ptr(G));
-    DQ_TRY(check_ptr(workspace, any));
+    DQ_TRY(check_ptr(workspace, d->tokens > kFew));
     DQ_TRY(check_device(P));
     hipStream_t st = static_cast<hipStream_t>(stream);
     const EmbedArgs a = args(P, d);
     const int64_t M = P->desc.M;
+    if (a.N <= kFew) {
+        if (!any && add) return DQGAN_OK;
+        const int64_t rows = few_rows(M, a.V, a.D);
+        with_type(d->type, [&](auto t) {
+            with_index(d->index_type, [&](auto i) {
+                using T = decltype(t);
+                using I = decltype(i);
+                k_embed_few<T, I><<<dim3(static_cast<uint32_t>(ceil_div(a.V, rows)), static_cast<uint32_t>(M)), 64 * kFewWaves, 0, st>>>(
+                    static_cast<const I *>(tok), static_cast<const T *>(dout), a, rows,
+                    slabs_of(a.D, Vec16<T>::kPer), width_of(a.D, Vec16<T>::kPer), G, add != 0);
+            });
+        });
+        return launched();
+    }
     const size_t list = list_bytes(M, a.N);
     uint32_t *key[2], *at[2];
     for (int i = 0; i < 2; ++i) {
@@ -583,13 +696,11 @@ dqgan_status dqgan_embed_backward(dqgan_plan P, const dqgan_embed_desc *d, const
     const int fills = add ? 0 : static_cast<int>(want < most ? want : most);
     const int runs = static_cast<int>(ceil_div(a.N, kRun)), sorts = static_cast<int>(M * runs);
     const int64_t groups = sorts + M * fills;
-    if (groups == 0) return DQGAN_OK;
     with_index(d->index_type, [&](auto i) {
         using I = decltype(i);
         k_embed_sort<I><<<static_cast<uint32_t>(groups), kSortThreads, 0, st>>>(
             static_cast<const I *>(tok), a, runs, sorts, digit, passes, key[0], at[0], fills, G);
     });
-    if (!any) return launched();
     int now = 0;
     for (int64_t len = kRun; len < a.N; len *= kFan, now ^= 1)
         k_embed_merge<<<dim3(static_cast<uint32_t>(ceil_div(a.N, 256)), static_cast<uint32_t>(M)), 256, 0, st>>>(

@@ -10,7 +10,8 @@ pytestmark = pytest.mark.gpu
 
 # M, tokens, vocabulary, width, offset
 SHAPES = [(1, 1, 1, 1, 0), (3, 1, 5, 7, 1), (2, 31, 2, 8, 4), (1, 32, 3, 9, 2), (2, 33, 40, 512, 0), (1, 64, 511, 513, 3),
-          (3, 65, 512, 64, 7), (1, 300, 513, 1, 0), (2, 1000, 37, 100, 5), (1, 1025, 70000, 17, 0), (2, 2500, 300, 1030, 9),
+          (3, 65, 512, 64, 7), (1, 300, 513, 1, 0), (2, 1000, 37, 100, 5), (3, 511, 700, 40, 1), (1, 512, 5, 1300, 0),
+          (2, 513, 30, 16, 6), (1, 200, 9000, 3, 0), (1, 40, 20, 40000, 1), (2, 63, 4000, 50, 3), (3, 64, 9, 1301, 0), (1, 1025, 70000, 17, 0), (2, 2500, 300, 1030, 9),
           (1, 5000, 4, 520, 0), (5, 0, 10, 12, 2), (1, 4096, 300, 3, 0), (2, 4097, 60, 9, 3), (1, 9000, 300001, 1, 2),
           (1, 66000, 5, 3, 0), (2, 140001, 3000, 2, 1)]
 

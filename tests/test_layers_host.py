@@ -52,7 +52,7 @@ OKP, ODD = 0x10000, 0x10008
 
 def _embed(**kw):
     from paper_2010_13359_amd import layers
-    base = dict(offset=10, vocab=50, width=20, tokens=7, scale=1.0, type=1, index_type=1, reserved=0)
+    base = dict(offset=10, vocab=50, width=20, tokens=1000, scale=1.0, type=1, index_type=1, reserved=0)
     base.update(kw)
     return layers.EmbedDesc(*base.values())
 
