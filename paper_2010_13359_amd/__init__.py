@@ -5,6 +5,8 @@ top-k), message packing, server average and the optimistic-mirror-descent
 update with the per-worker extrapolated point.
 
 The computation lives in the HIP library ``libdqgan.so`` behind the C ABI of
-``include/dqgan.h``; ``dqgan`` is its Python binding.
+``include/dqgan.h`` and ``include/dqgan_layers.h``; ``dqgan`` and ``layers``
+are its Python bindings (the iteration, and the layers that turn evaluation
+points into gradients).
 """
-from . import dqgan  # noqa: F401
+from . import dqgan, layers  # noqa: F401

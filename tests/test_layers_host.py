@@ -141,3 +141,18 @@ def test_pointers(lib):
     # the parameters' row stride: the plan's or 0
     assert lib.dqgan_embed_forward(p.handle, e, OKP, OKP, 5000, OKP, None) == -1
     assert lib.dqgan_norm_forward(p.handle, n, OKP, OKP, 1024, OKP, OKP, None) == -1
+
+
+def test_header_is_plain_c(tmp_path):
+    """include/dqgan_layers.h compiles as C11 and its functions link."""
+    import subprocess
+    from paper_2010_13359_amd import layers
+    c = tmp_path / "uses.c"
+    c.write_text('#include "dqgan_layers.h"\nint main(void) {\n' + "".join(
+        "    if ((void *)%s == 0) return 1;\n" % n for n in layers.EXPORTS) + "    return 0;\n}\n")
+    pkg = os.path.join(ROOT, "paper_2010_13359_amd")
+    r = subprocess.run(["gcc", "-std=c11", "-Wall", "-Wextra", "-Werror", "-Wno-address", "-I", os.path.join(ROOT, "include"),
+                        str(c), "-o", str(tmp_path / "uses"), "-L", pkg, "-ldqgan", "-L", "/opt/rocm/lib", "-lamdhip64",
+                        "-Wl,-rpath," + pkg + ":/opt/rocm/lib"], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout + r.stderr
+    assert subprocess.run([str(tmp_path / "uses")], timeout=100).returncode == 0
