@@ -45,15 +45,46 @@ struct Softmax {
 // the student's logits there, and t and log t.
 struct Message {
     uint32_t idx[kMostEntries];
-    float z[kMostEntries], t[kMostEntries], logt[kMostEntries];
+    float z[kMostEntries];
+    union {
+        struct {
+            float t[kMostEntries], logt[kMostEntries];
+        };
+        uint32_t seen[2 * kMostEntries];  // before them: the indices by their hash
+    };
     float slots[4][16];
 };
 
+// Whether an index comes twice among the message's.  Every thread calls it.
+template <int W>
+__device__ bool repeats(int k, Message &s) {
+    const int bits = 33 - __builtin_clz(k - 1 | 1);  // at least twice k places
+    const uint32_t last = (1u << bits) - 1;
+    for (uint32_t i = threadIdx.x; i <= last; i += 64 * W) s.seen[i] = UINT32_MAX;
+    __syncthreads();
+    bool twice = false;
+    for (int j = threadIdx.x; j < k; j += 64 * W) {
+        const uint32_t i = s.idx[j];
+        if (i == UINT32_MAX) continue;
+        for (uint32_t h = i * 2654435769u >> (32 - bits);; h = (h + 1) & last) {
+            const uint32_t there = atomicCAS(&s.seen[h], UINT32_MAX, i);
+            twice |= there == i;
+            if (there == i || there == UINT32_MAX) break;
+        }
+    }
+    return __syncthreads_or(twice) != 0;
+}
+
 // Reads a message and the student's logits at its entries (those that lie in
 // columns [begin, end), or all of them from `gathered`), and makes t and log t.
-// Every thread of the workgroup calls it.  Returns 0 if no entry counts, 1 if
-// their indices ascend (so that none comes twice), else 2.
-template <typename T, int W>
+// Every thread of the workgroup calls it.  Returns 0 if no entry counts, 2 if an
+// index may come twice (of interest for GRAD), else 1: at once if they ascend,
+// otherwise by their hash.  Loss and gradient of 4096 x 2000 bf16 logits with
+// messages in no order, of 16 entries 15.5 us where each entry looks at all
+// others and 16.4 with a hash; of 64 19.9 and 17.0, of 256 49 and 20.8, of 1024
+// 551 and 35.6.
+constexpr int kLookAtAll = 32;
+template <typename T, int W, bool GRAD>
 __device__ int teacher(const DistillArgs &a, int64_t row, const T *z, const float *gathered, int64_t begin, int64_t end,
                        Message &s) {
     const float *val = a.val + row * a.k;
@@ -76,6 +107,11 @@ __device__ int teacher(const DistillArgs &a, int64_t row, const T *z, const floa
             s.z[j] = static_cast<float>(z[i]);
     }
     have = (__syncthreads_or(have & 1) ? 1 : 0) | (__syncthreads_or(have & 2) ? 2 : 0);
+    bool twice = have == 3;
+    if (GRAD && twice && a.k > kLookAtAll) {
+        twice = repeats<W>(a.k, s);
+        for (int j = threadIdx.x; j < a.k; j += 64 * W) s.t[j] = val[j];
+    }
     top = group_max<W>(top, s.slots[0]);
     float sum = 0.0f;
     for (int j = threadIdx.x; j < a.k; j += 64 * W) {
@@ -92,7 +128,7 @@ __device__ int teacher(const DistillArgs &a, int64_t row, const T *z, const floa
         s.t[j] /= sum;
     }
     __syncthreads();
-    return (have & 1) == 0 ? 0 : (have & 2) ? 2 : 1;
+    return (have & 1) == 0 ? 0 : twice ? 2 : 1;
 }
 
 // The loss of a token that takes part.  Every thread calls it.
@@ -213,7 +249,7 @@ __global__ __launch_bounds__(64 * W) void k_distill_row(const T *z, DistillArgs 
     Logits<T, W, NV, STREAM> l;
     if (weight != 0.0f) {
         l.load(from, vectors, rest);
-        have = teacher<T, W>(a, row, from, nullptr, 0, a.V, s);
+        have = teacher<T, W, GRAD>(a, row, from, nullptr, 0, a.V, s);
     }
     if (have != 0) {
         if (LOSS) {
@@ -295,7 +331,7 @@ __global__ __launch_bounds__(256) void k_distill_slice(const T *z, DistillArgs a
     Logits<T, 4, kSliceVectors, false> l;
     if (weight != 0.0f) {
         if (GRAD) l.load(from + begin, vectors, rest);
-        have = teacher<T, 4>(a, row, from, LOSS ? gathered + row * a.k : nullptr, begin, begin + n, s);
+        have = teacher<T, 4, GRAD>(a, row, from, LOSS ? gathered + row * a.k : nullptr, begin, begin + n, s);
     }
     if (have != 0) {
         if (LOSS) {
@@ -373,9 +409,12 @@ int64_t slices_of(int64_t bytes) { return ceil_div(bytes, 64 * 4 * kSliceVectors
 // Whether long rows (16 vectors a lane) pass by the caches: loss and gradient of
 // 32000 bf16 logits, read and written, of 33 MB in all 11.5 us so and 11.9
 // with ordinary accesses, of 132 MB 28.6 / 33.1, 526 MB 102 / 115; of 128000
-// logits 8 MB 20.7 / 18.8, 1050 MB 221 / 236, 2500 MB 580 / 563.
+// logits 8 MB 20.7 / 18.8, 1050 MB 221 / 236, 2500 MB 580 / 563.  Entries are
+// written into the row once more: not if there are as many as lines of 128 bytes
+// (526 MB, 256 entries 117 / 137, 1024 233 / 170).
 constexpr double kStreamFrom = 64e6, kStreamUpTo = 1.4e9;
-bool streams(int64_t rows, int64_t bytes) {
+bool streams(int64_t rows, int64_t bytes, int k) {
+    if (k > bytes / 128) return false;
     const double total = 2.0 * static_cast<double>(rows) * static_cast<double>(bytes);
     return total >= kStreamFrom && total <= kStreamUpTo;
 }
@@ -448,7 +487,7 @@ dqgan_status run(dqgan_plan P, const dqgan_distill_desc *d, const void *z, const
             float *l = loss ? loss + r : loss, *x = stats ? stats + 2 * r : stats;
             with_shape(bytes, [&](auto w, auto nv) {
                 constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-                if (GRAD && NV == 16 && streams(rows, bytes))
+                if (GRAD && NV == 16 && streams(rows, bytes, d->k))
                     k_distill_row<T, W, NV, LOSS, GRAD, GRAD && NV == 16><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
                 else
                     k_distill_row<T, W, NV, LOSS, GRAD, false><<<n, 64 * W, 0, st>>>(from, b, l, x, to);

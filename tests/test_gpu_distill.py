@@ -139,6 +139,25 @@ def test_repeated_entries():
     pl.close()
 
 
+@pytest.mark.parametrize("k", [2, 32, 33, 200, 1024])
+@pytest.mark.parametrize("V", [3000, 140000])
+def test_messages_in_any_order(V, k):
+    """Distinct indices in no order, one pair of equal ones among them, skipped
+    entries between, and indices close together or at steps of a Fibonacci number."""
+    import torch
+    pl, z, val, idx, weight = _setup((1, 5, V, 0, k), "bf16", seed=k)
+    gen = torch.Generator().manual_seed(V + k)
+    idx[0, 0] = torch.randperm(V, generator=gen)[:k].int()
+    idx[0, 1] = idx[0, 0]
+    idx[0, 1, 0] = idx[0, 1, k - 1]
+    idx[0, 2] = idx[0, 0]
+    idx[0, 2, ::3] = -1
+    idx[0, 3] = (V - 1 - torch.arange(k)).int()
+    idx[0, 4] = (torch.arange(k) * 2584 % V).flip(0).int()
+    _compare(z, val, idx, weight, V, 1.0, _run(pl, z, val, idx, weight, V, 1.0))
+    pl.close()
+
+
 def test_nan_and_infinity_spread_over_their_token_only():
     import torch
     for V in (500, 70000, 140000):
