@@ -22,7 +22,6 @@
 namespace dq {
 namespace {
 
-constexpr int kChunk = 32;                 // sorted places per wave of k_embed_sum (at most 64)
 constexpr int kRun = 4096;                 // tokens per workgroup of k_embed_sort
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kEach = kRun / kSortThreads;
 constexpr int kDigitMost = 9;              // bits of a sort digit: 512 counters for each of 16 waves
@@ -382,44 +381,84 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_embed_few(const I *tok, cons
     }
 }
 
-template <typename T, bool STREAM>
+// A task is CHUNK sorted places and one slab of the row, done by L lanes.
+template <typename T, int L, int CHUNK, bool STREAM>
 __global__ __launch_bounds__(256) void k_embed_sum(const uint32_t *key, const uint32_t *at, const T *dout, EmbedArgs a,
                                                    int64_t chunks, int slabs, int width, float *part, float *G, bool add) {
-    static_assert(2 * kChunk <= 64, "a lane for each place of a chunk and the next");
-    const int64_t m = blockIdx.y, task = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    constexpr int kSeen = 2 * CHUNK, kGroups = 256 / L;  // places of a chunk and the next
+    constexpr bool kWave = L == 64;
+    static_assert(kSeen <= 64 && (kWave || kSeen % L == 0), "a bit for each place");
+    __shared__ uint32_t keys[kWave ? 1 : kGroups][kWave ? 1 : kSeen], places[kWave ? 1 : kGroups][kWave ? 1 : kSeen];
+    const int64_t m = blockIdx.y, task = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / L;
     if (task >= chunks * slabs) return;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
     const int64_t chunk = task / slabs;
     const Channels<T> ch(a.D, static_cast<int>(task % slabs), slabs, width, lane);
-    const int64_t e0 = chunk * kChunk;
+    const int64_t e0 = chunk * CHUNK;
     key += m * a.N;
     at += m * a.N;
     dout += m * a.N * a.D;
     G += m * a.ld + a.offset;
     part += (m * chunks + chunk) * 2 * a.D;
     const uint32_t V = static_cast<uint32_t>(a.V);
-    // lane i: place e0 + i of this chunk and the next, and whether its token ends there
-    const uint32_t k = e0 + lane < a.N ? key[e0 + lane] : V;
-    const uint32_t where = e0 + lane < a.N ? at[e0 + lane] : 0;
     const uint32_t before = e0 > 0 ? key[e0 - 1] : V;
-    const uint32_t earlier = e0 > kChunk ? key[e0 - kChunk - 1] : V;  // the last place before the chunk before
-    const uint32_t behind = e0 + 2 * kChunk < a.N ? key[e0 + 2 * kChunk] : V;
-    uint32_t next = __shfl_down(k, 1);
-    if (lane == 2 * kChunk - 1) next = behind;
-    const uint64_t ends = __ballot(k != next);
-    const int valid = __popcll(__ballot(k != V));  // padded places come last
-    const uint32_t head = __builtin_amdgcn_readlane(k, 0);
+    const uint32_t earlier = e0 > CHUNK ? key[e0 - CHUNK - 1] : V;  // the last place before the chunk before
+    const uint32_t behind = e0 + kSeen < a.N ? key[e0 + kSeen] : V;
+    // bit i: the token at place e0 + i ends there; is none (padded places come last)
+    uint64_t ends = 0, none = 0;
+    uint32_t k = V, where = 0;
+    if constexpr (kWave) {  // lane i: place e0 + i
+        k = e0 + lane < a.N ? key[e0 + lane] : V;
+        where = e0 + lane < a.N ? at[e0 + lane] : 0;
+        uint32_t next = __shfl_down(k, 1);
+        if (lane == kSeen - 1) next = behind;
+        ends = __ballot(k != next);
+        none = __ballot(k == V);
+    } else {
+        constexpr int kEach = kSeen / L;
+        uint32_t mine[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int64_t e = e0 + L * j + lane;
+            mine[j] = e < a.N ? key[e] : V;
+            places[group][L * j + lane] = e < a.N ? at[e] : 0;
+            keys[group][L * j + lane] = mine[j];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // a group lies in one wave
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const uint32_t across = j + 1 < kEach ? __shfl(mine[j + 1 < kEach ? j + 1 : j], 0, L) : behind;
+            uint32_t next = __shfl_down(mine[j], 1, L);
+            if (lane == L - 1) next = across;
+            const int base = (threadIdx.x & 63) / L * L;
+            ends |= (__ballot(mine[j] != next) >> base & ((uint64_t(1) << L) - 1)) << (L * j);
+            none |= (__ballot(mine[j] == V) >> base & ((uint64_t(1) << L) - 1)) << (L * j);
+        }
+    }
+    if constexpr (kSeen < 64) {
+        ends &= (uint64_t(1) << kSeen) - 1;
+        none |= ~uint64_t(0) << kSeen;
+    }
+    const auto key_at = [&](int e) {
+        return kWave ? static_cast<uint32_t>(__builtin_amdgcn_readlane(k, e)) : keys[kWave ? 0 : group][kWave ? 0 : e];
+    };
+    const auto place_at = [&](int e) {
+        return kWave ? static_cast<uint32_t>(__builtin_amdgcn_readlane(where, e)) : places[kWave ? 0 : group][kWave ? 0 : e];
+    };
+    const int valid = __popcll(~none);
+    const uint32_t head = key_at(0);
     // places of the token that began in an earlier chunk, and whether it was that chunk's to finish
     const int led = head != V && head == before ? (ends != 0 ? __ffsll(static_cast<long long>(ends)) : 65) : 0;
-    const bool finished = led <= kChunk && earlier != head;
+    const bool finished = led <= CHUNK && earlier != head;
     int first = led > 0 && finished ? led : 0;
     bool leading = led > 0 && !finished;  // its partial sum comes first
     // to the end of the last token that begins here, if that is in sight
-    int n = valid < kChunk ? valid : kChunk;
-    if (n == kChunk && !(ends >> (kChunk - 1) & 1)) {
-        const bool mine = !(leading && led > kChunk);  // it begins here
-        const uint64_t later = ends >> kChunk;
-        if (mine && later != 0) n = kChunk + __ffsll(static_cast<long long>(later));
+    int n = valid < CHUNK ? valid : CHUNK;
+    if (n == CHUNK && !(ends >> (CHUNK - 1) & 1)) {
+        const bool mine = !(leading && led > CHUNK);  // it begins here
+        const uint64_t later = ends >> CHUNK;
+        if (mine && later != 0) n = CHUNK + __ffsll(static_cast<long long>(later));
     }
     typename Vec16<T>::wide s = 0.0f;
     float t = 0.0f;
@@ -428,10 +467,8 @@ __global__ __launch_bounds__(256) void k_embed_sum(const uint32_t *key, const ui
         typename Vec16<T>::type raw[kBatch];
         typename Bits<T>::type last[kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const int e = b + u < n ? b + u : b;  // beyond n: this batch's first row once more
-            row[u] = dout + static_cast<int64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(where, e))) * a.D;
-        }
+        for (int u = 0; u < kBatch; ++u)  // beyond n: this batch's first row once more
+            row[u] = dout + static_cast<int64_t>(place_at(b + u < n ? b + u : b)) * a.D;
         if (ch.some_whole) {
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) raw[u] = load16<T, STREAM>(row[u] + ch.from);
@@ -448,8 +485,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const uint32_t *key, const ui
             const bool end = ends >> (b + u) & 1;
             if (!end && b + u + 1 < n) continue;
             if (!leading && end)
-                ch.put(G + static_cast<int64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(k, b + u))) * a.D, s, t,
-                       a.scale, add);
+                ch.put(G + static_cast<int64_t>(key_at(b + u)) * a.D, s, t, a.scale, add);
             else
                 ch.leave(part + (leading ? 0 : a.D), s, t);
             s = 0.0f;
@@ -465,7 +501,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const uint32_t *key, const ui
 // chunk, then take such tokens in turn; one of many chunks is shared out among
 // them.
 constexpr int kJoinWaves = 8, kJoinChunks = 16, kMany = 2 * kBatch;
-template <typename T>
+template <typename T, int CHUNK>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(const uint32_t *key, EmbedArgs a, int64_t chunks, int slabs,
                                                                 int width, const float *part, float *G, bool add) {
     __shared__ float sums[kJoinWaves][64][Vec16<T>::kPer + 1], tails[kJoinWaves][64];
@@ -476,12 +512,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(const uint32_t *
     G += m * a.ld + a.offset;
     part += m * chunks * 2 * a.D;
     const uint32_t V = static_cast<uint32_t>(a.V);
-    const int64_t e0 = (from + lane) * kChunk, e1 = e0 + kChunk;
+    const int64_t e0 = (from + lane) * CHUNK, e1 = e0 + CHUNK;
     bool begins = false;  // a token begins in chunk from + lane and runs on
     uint32_t k = V;
     if (lane < kJoinChunks && e1 < a.N) {
         k = key[e1 - 1];
-        begins = e1 + kChunk < a.N && k != V && key[e1 + kChunk] == k && !(e0 > 0 && key[e0 - 1] == k);
+        begins = e1 + CHUNK < a.N && k != V && key[e1 + CHUNK] == k && !(e0 > 0 && key[e0 - 1] == k);
     }
     const Channels<T> ch(a.D, static_cast<int>(blockIdx.x % slabs), slabs, width, lane);
     uint64_t todo = __ballot(begins);
@@ -492,7 +528,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(const uint32_t *
         // chunks that begin with this token: 64 looked at in one go
         int64_t last = chunk + 1;
         for (;;) {
-            const int64_t first = (last + lane) * kChunk;
+            const int64_t first = (last + lane) * CHUNK;
             const uint64_t others = ~__ballot(first < a.N && key[first < a.N ? first : 0] == token);
             if (others != 0) {
                 last += __ffsll(static_cast<long long>(others)) - 1;
@@ -552,13 +588,38 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(const uint32_t *
 
 constexpr int64_t kMostGroups = int64_t(1) << 24;  // of 256 threads in a launch's first dimension: below 2^32 threads
 
-int64_t chunks_of(int64_t N) { return ceil_div(N, kChunk); }
 // The vectors of a row in equal shares of up to 64, one per wave.
 int slabs_of(int64_t D, int per) {
     const int64_t s = ceil_div(D / per, 64);
     return static_cast<int>(s < 1 ? 1 : s);
 }
 int width_of(int64_t D, int per) { return static_cast<int>(ceil_div(D / per, slabs_of(D, per))); }
+
+constexpr int kChunkLong = 32, kChunkShort = 8;
+// Sorted places per wave of k_embed_sum: few where its waves would be up to four
+// per CU.  Whole gradients (bf16, M x N tokens, V x D), us with 32 and with 8:
+// 1 x 256, 3000 x 64 22.2 / 16.3; 1 x 2048, 3000 x 768 28.3 / 20.9; 8 x 2048,
+// 3000 x 512 33.5 / 28.4; 1 x 16384, 3000 x 768 43.0 / 39.3; behind the bound 2 x
+// 20000, 1000 x 1024 51.3 / 57.4, 32 x 4096, 1000 x 64 36.9 / 50.9.
+int chunk_of(int64_t M, const dqgan_embed_desc *d) {
+    const int64_t waves = M * ceil_div(d->tokens, kChunkLong) * slabs_of(d->width, d->type == DQGAN_F32 ? 4 : 8);
+    return waves <= 1024 ? kChunkShort : kChunkLong;
+}
+// f(L, CHUNK): of rows of up to 256 bytes a wave sums several chunks.  16 x 65536
+// tokens, 3000 x 128 bf16 204 us a wave a chunk and 180 so, of 3000 x 64 196 and
+// 152; 32 lanes a chunk of 512 byte rows made no difference.
+template <typename F>
+void with_task(int chunk, int width, F &&f) {
+    using std::integral_constant;
+    if (chunk == kChunkShort)
+        f(integral_constant<int, 64>{}, integral_constant<int, kChunkShort>{});
+    else if (width <= 8)
+        f(integral_constant<int, 8>{}, integral_constant<int, kChunkLong>{});
+    else if (width <= 16)
+        f(integral_constant<int, 16>{}, integral_constant<int, kChunkLong>{});
+    else
+        f(integral_constant<int, 64>{}, integral_constant<int, kChunkLong>{});
+}
 
 // Rows of a workgroup of k_embed_few: 8 to 128 KB of G, to fill the card.
 int64_t few_rows(int64_t M, int64_t V, int64_t D) {
@@ -576,7 +637,7 @@ dqgan_status check(dqgan_plan P, const dqgan_embed_desc *d) {
     if (d->offset < 0 || d->offset >= n || d->vocab > (n - d->offset) / d->width) return DQGAN_EINVAL;
     if (!tokens_ok(P, d->tokens) || !type_ok(d->type) || d->reserved != 0 || !isfinite(d->scale)) return DQGAN_EINVAL;
     if (d->index_type != DQGAN_I32 && d->index_type != DQGAN_I64) return DQGAN_EINVAL;
-    if (chunks_of(d->tokens) * slabs_of(d->width, 4) > kMostGroups) return DQGAN_EINVAL;
+    if (ceil_div(d->tokens, kChunkLong) * slabs_of(d->width, 4) > kMostGroups) return DQGAN_EINVAL;
     return DQGAN_OK;
 }
 
@@ -650,7 +711,7 @@ dqgan_status dqgan_embed_bytes(dqgan_plan P, const dqgan_embed_desc *d, size_t *
     const int64_t M = P->desc.M;
     *bytes = d->tokens <= kFew ? 0
                             : 2 * pairs_of(d->tokens) * list_bytes(M, d->tokens) +
-                                  sizeof(float) * 2 * static_cast<size_t>(M * chunks_of(d->tokens)) * d->width;
+                                  sizeof(float) * 2 * static_cast<size_t>(M * ceil_div(d->tokens, chunk_of(M, d))) * d->width;
     return DQGAN_OK;
 }
 
@@ -705,19 +766,23 @@ dqgan_status dqgan_embed_backward(dqgan_plan P, const dqgan_embed_desc *d, const
     for (int64_t len = kRun; len < a.N; len *= kFan, now ^= 1)
         k_embed_merge<<<dim3(static_cast<uint32_t>(ceil_div(a.N, 256)), static_cast<uint32_t>(M)), 256, 0, st>>>(
             key[now], at[now], static_cast<int>(a.N), static_cast<int>(len), key[now ^ 1], at[now ^ 1]);
-    const int64_t chunks = chunks_of(a.N);
+    const int chunk = chunk_of(M, d);
+    const int64_t chunks = ceil_div(a.N, chunk);
     with_type(d->type, [&](auto t) {
         using T = decltype(t);
         const int slabs = slabs_of(a.D, Vec16<T>::kPer), width = width_of(a.D, Vec16<T>::kPer);
         const uint32_t my = static_cast<uint32_t>(M);
-        with_stream(backward_streams(static_cast<double>(sizeof(T)) * M * a.N * a.D), [&](auto streams) {
-            k_embed_sum<T, decltype(streams)::value>
-                <<<dim3(static_cast<uint32_t>(ceil_div(chunks * slabs, 4)), my), 256, 0, st>>>(
+        with_task(chunk, width, [&](auto l, auto c) {
+            constexpr int L = decltype(l)::value, C = decltype(c)::value;
+            const dim3 grid(static_cast<uint32_t>(ceil_div(chunks * slabs, 256 / L)), my);
+            with_stream(backward_streams(static_cast<double>(sizeof(T)) * M * a.N * a.D), [&](auto streams) {
+                k_embed_sum<T, L, C, decltype(streams)::value><<<grid, 256, 0, st>>>(
                     key[now], at[now], static_cast<const T *>(dout), a, chunks, slabs, width, part, G, add != 0);
+            });
+            if (chunks > 2)
+                k_embed_join<T, C><<<dim3(static_cast<uint32_t>(ceil_div(chunks, kJoinChunks) * slabs), my), 64 * kJoinWaves, 0,
+                                     st>>>(key[now], a, chunks, slabs, width, part, G, add != 0);
         });
-        if (chunks > 2)
-            k_embed_join<T><<<dim3(static_cast<uint32_t>(ceil_div(chunks, kJoinChunks) * slabs), my), 64 * kJoinWaves, 0, st>>>(
-                key[now], a, chunks, slabs, width, part, G, add != 0);
     });
     return launched();
 }
