@@ -25,7 +25,7 @@ namespace {
 constexpr int kRun = 4096;                 // tokens per workgroup of k_embed_sort
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kEach = kRun / kSortThreads;
 constexpr int kDigitMost = 9;              // bits of a sort digit: 512 counters for each of 16 waves
-constexpr int kFan = 16;
+constexpr int kFan = 4;
 constexpr int64_t kFillFloats = 32768;     // of G per workgroup
 
 struct EmbedArgs {
@@ -200,13 +200,15 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(const I *tok, Embed
 // Runs of `len` places (at least a workgroup's 256) to runs of kFan * len: a
 // token's new place is its place in its run plus, for each other run, how many of
 // its tokens come before.  A wave holds 64 neighbours of a sorted run: first its
-// lanes search for its first and its last token, four lanes a run, each of which
-// looks at one of the four places that cut what is left in five; the other
-// tokens' counts lie between those two, most often a few places apart.  Every
-// step waits for memory, so searches go side by side.
+// lanes search for its first and its last token, 16 lanes a run, each of which
+// looks at one of the 16 places that cut what is left in 17; the other tokens'
+// counts lie between those two, most often some 64 places apart.  Every step waits
+// for memory, so searches go side by side.  65536 tokens: two launches of 7.5 us,
+// of 16 workers 23 us each; one launch that joins 16 runs 17.8 and 73.
 __global__ __launch_bounds__(256) void k_embed_merge(const uint32_t *key, const uint32_t *at, int N, int len,
                                                      uint32_t *to_key, uint32_t *to_at) {
-    static_assert(kFan == 16, "four lanes a run");
+    constexpr int kCuts = 64 / kFan;  // lanes a run
+    constexpr uint64_t kEachRun = ~uint64_t(0) / ((uint64_t(1) << kFan) - 1);  // every kFan-th bit
     const int first = static_cast<int>(blockIdx.x) * 256, i = first + threadIdx.x, lane = threadIdx.x & 63;
     const int64_t m = blockIdx.y;
     key += m * N;
@@ -214,9 +216,9 @@ __global__ __launch_bounds__(256) void k_embed_merge(const uint32_t *key, const 
     const int run = first / len, group = run / kFan * kFan;
     const bool in = i < N;
     const uint32_t k = key[in ? i : N - 1], where = at[in ? i : N - 1];
-    uint32_t ends[2] = {0, 0};  // counts of the wave's first and last token in run group + lane % 16
+    uint32_t ends[2] = {0, 0};  // counts of the wave's first and last token in run group + lane % kFan
     {
-        const int r = lane & 15, j = lane >> 4;
+        const int r = lane % kFan, j = lane / kFan;
         const int64_t begin = static_cast<int64_t>(group + r) * len;
         const uint32_t here = begin >= N || group + r == run ? 0 : static_cast<uint32_t>(N - begin < len ? N - begin : len);
         const uint32_t mine[2] = {static_cast<uint32_t>(__builtin_amdgcn_readlane(k, 0)) + (group + r < run),
@@ -226,16 +228,15 @@ __global__ __launch_bounds__(256) void k_embed_merge(const uint32_t *key, const 
             bool before[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const uint32_t cut = ends[e] + static_cast<uint32_t>(uint64_t(j + 1) * (left[e] + 1) / 5);
+                const uint32_t cut = ends[e] + static_cast<uint32_t>(uint64_t(j + 1) * (left[e] + 1) / (kCuts + 1));
                 before[e] = cut <= ends[e] || key[begin + cut - 1] < mine[e];
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const uint64_t votes = __ballot(before[e]) >> r;  // bits 0, 16, 32, 48: this run's four
-                const int yes = (votes & 1) + (votes >> 16 & 1) + (votes >> 32 & 1) + (votes >> 48 & 1);
+                const int yes = __popcll(__ballot(before[e]) >> r & kEachRun);  // of this run's lanes
                 const uint32_t n = left[e], low = ends[e];
-                if (yes > 0) ends[e] = low + static_cast<uint32_t>(uint64_t(yes) * (n + 1) / 5);
-                const uint32_t high = yes < 4 ? low + static_cast<uint32_t>(uint64_t(yes + 1) * (n + 1) / 5) - 1 : low + n;
+                if (yes > 0) ends[e] = low + static_cast<uint32_t>(uint64_t(yes) * (n + 1) / (kCuts + 1));
+                const uint32_t high = yes < kCuts ? low + static_cast<uint32_t>(uint64_t(yes + 1) * (n + 1) / (kCuts + 1)) - 1 : low + n;
                 left[e] = high - ends[e];
             }
         }
@@ -299,15 +300,18 @@ struct Channels {
 };
 
 constexpr int kBatch = 8;
-// Against the launches of more, 128 tokens for each of M workers' tables of V x D
-// (bf16): 1 x 1000 x 1024 8.4 and 22.4 us, 1 x 32000 x 1024 25.4 and 41.7, 8 x 150 x 64
-// 11.3 and 19.0, 16 x 30000 x 64 34.9 and 40.7; 256 tokens 8.3 and 22.8, 28.0 and
-// 41.7, 16.6 and 19.8, 47.0 and 41.2, as a row's tokens are added one after the other.
+// Workgroups of all workers' first rows come first: tokens of low number are the
+// frequent ones in most vocabularies, and their sums take longest (16 workers, 192
+// tokens, 30000 x 64 29.8 us so and 39 worker by worker).  Against the launches of
+// more, 192 tokens for each of M workers' tables of V x D (bf16): 1 x 1000 x 1024
+// 8.4 and 16.7 us, 1 x 32000 x 1024 26.9 and 34.3, 8 x 150 x 64 13.8 and 16.0, 26 x
+// 53776 x 77 85 and 92, 16 x 30000 x 64 29.8 and 34.3.  A token that comes
+// N times is N rows one after the other, so that more are not better off here.
 constexpr int kFewRounds = 3, kFew = 64 * kFewRounds, kFewWaves = 8, kFewBatch = 4;
 template <typename T, typename I>
-__global__ __launch_bounds__(64 * kFewWaves) void k_embed_few(const I *tok, const T *dout, EmbedArgs a, int64_t rows,
-                                                              int slabs, int width, float *G, bool add) {
-    const int64_t m = blockIdx.y, row0 = static_cast<int64_t>(blockIdx.x) * rows;
+__global__ __launch_bounds__(64 * kFewWaves) void k_embed_few(const I *tok, const T *dout, EmbedArgs a, uint32_t workers,
+                                                              int64_t rows, int slabs, int width, float *G, bool add) {
+    const int64_t m = blockIdx.x % workers, row0 = static_cast<int64_t>(blockIdx.x / workers) * rows;
     const int64_t mine = a.V - row0 < rows ? a.V - row0 : rows;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     dout += m * a.N * a.D;
@@ -496,91 +500,121 @@ __global__ __launch_bounds__(256) void k_embed_sum(const uint32_t *key, const ui
 }
 
 // Tokens that run on beyond the chunk after the one they begin in: that chunk's
-// second partial sum and the first ones of those that follow, in this order.  One workgroup per
-// kJoinChunks chunks and slab: its waves look at the chunks' borders, one lane a
-// chunk, then take such tokens in turn; one of many chunks is shared out among
-// them.
-constexpr int kJoinWaves = 8, kJoinChunks = 16, kMany = 2 * kBatch;
-template <typename T, int CHUNK>
+// second partial sum and the first ones of those that follow, in this order.  One
+// workgroup per kJoinChunks chunks and slab: its waves look at one chunk's border
+// each and how far the token there goes; then its groups of L lanes take one such
+// token each, and one of many chunks is shared out among them (a million places of
+// one token, rows of 64 bf16: the whole gradient 208 us, and 846 when a wave took
+// all its lanes for one partial sum and the token's chunks were counted 64 by 64).
+constexpr int kJoinWaves = 8, kJoinChunks = kJoinWaves, kMany = 2 * kBatch;
+template <typename T, int L, int CHUNK>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(const uint32_t *key, EmbedArgs a, int64_t chunks, int slabs,
-                                                                int width, const float *part, float *G, bool add) {
-    __shared__ float sums[kJoinWaves][64][Vec16<T>::kPer + 1], tails[kJoinWaves][64];
+                                                                   int width, const float *part, float *G, bool add) {
+    constexpr int kGroups = 64 * kJoinWaves / L, kPer = Vec16<T>::kPer, kAhead = (L == 64 ? 32 : 16) / kPer;
+    static_assert(kJoinChunks <= kGroups, "a group for each token");
+    __shared__ float sums[kGroups][L][kPer + 1], tails[kGroups][L];
+    __shared__ int counts[kJoinChunks];  // chunks that begin with the token; 0: no such token
+    __shared__ uint32_t tokens[kJoinChunks];
     typedef typename Vec16<T>::wide Wide;
     const int64_t m = blockIdx.y, from = static_cast<int64_t>(blockIdx.x / slabs) * kJoinChunks;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
     key += m * a.N;
     G += m * a.ld + a.offset;
     part += m * chunks * 2 * a.D;
     const uint32_t V = static_cast<uint32_t>(a.V);
-    const int64_t e0 = (from + lane) * CHUNK, e1 = e0 + CHUNK;
-    bool begins = false;  // a token begins in chunk from + lane and runs on
-    uint32_t k = V;
-    if (lane < kJoinChunks && e1 < a.N) {
-        k = key[e1 - 1];
-        begins = e1 + CHUNK < a.N && k != V && key[e1 + CHUNK] == k && !(e0 > 0 && key[e0 - 1] == k);
-    }
-    const Channels<T> ch(a.D, static_cast<int>(blockIdx.x % slabs), slabs, width, lane);
-    uint64_t todo = __ballot(begins);
-    for (int turn = 0; todo != 0; todo &= todo - 1, ++turn) {
-        const int l = __ffsll(static_cast<long long>(todo)) - 1;
-        const int64_t chunk = from + l;
-        const uint32_t token = __builtin_amdgcn_readlane(k, l);
-        // chunks that begin with this token: 64 looked at in one go
-        int64_t last = chunk + 1;
-        for (;;) {
-            const int64_t first = (last + lane) * CHUNK;
-            const uint64_t others = ~__ballot(first < a.N && key[first < a.N ? first : 0] == token);
-            if (others != 0) {
-                last += __ffsll(static_cast<long long>(others)) - 1;
-                break;
+    {
+        const int wave = threadIdx.x >> 6, probe = threadIdx.x & 63;
+        const int64_t chunk = from + wave, e0 = chunk * CHUNK, e1 = e0 + CHUNK;
+        int n = 0;
+        uint32_t token = V;
+        if (e1 + CHUNK < a.N) {
+            token = key[e1 - 1];
+            if (token != V && key[e1 + CHUNK] == token && !(e0 > 0 && key[e0 - 1] == token)) {
+                // the first chunk that does not begin with it: 64 looked at in one go, apart
+                // by steps that grow till one is past the token's end and then shrink
+                int64_t last = chunk + 2;  // the one before begins with it
+                for (int64_t step = 1;;) {
+                    const int64_t e = (last + probe * step) * CHUNK;
+                    const uint64_t others = ~__ballot(e < a.N && key[e < a.N ? e : 0] == token);
+                    if (others == 0) {
+                        last += 63 * step + 1;
+                        step *= 64;
+                        continue;
+                    }
+                    const int p = __ffsll(static_cast<long long>(others)) - 1;
+                    if (step == 1 || p == 0) {
+                        last += p;
+                        break;
+                    }
+                    last += (p - 1) * step + 1;
+                    step /= 64;
+                }
+                n = static_cast<int>(last - chunk - 1);
             }
-            last += 64;
         }
-        const int64_t n = last - chunk - 1;
-        const bool shared = n > kMany;  // the same for the whole workgroup
-        if (!shared && turn % kJoinWaves != wave) continue;
-        const int64_t each = shared ? (n + kJoinWaves - 1) / kJoinWaves : n;
-        const int64_t first = chunk + 1 + (shared ? wave * each : 0), upto = first + each < last ? first + each : last;
-        Wide s = 0.0f;
-        float t = 0.0f;
-        if (!shared || wave == 0) {
-            const float *p = part + (2 * chunk + 1) * a.D;
-            if (ch.whole) s = load_floats<T>(p + ch.c);
-            if (ch.tail) t = p[ch.ct];
+        if (probe == 0) {
+            counts[wave] = n;
+            tokens[wave] = token;
         }
-        for (int64_t b = first; b < upto; b += kBatch) {
+    }
+    __syncthreads();
+    const Channels<T> ch(a.D, static_cast<int>(blockIdx.x % slabs), slabs, width, lane);
+    Wide s = 0.0f;
+    float t = 0.0f;
+    // the second partial sum of chunk c and the first ones of chunks [first, upto)
+    const auto begin = [&](int64_t c) {
+        const float *p = part + (2 * c + 1) * a.D;
+        if (ch.whole) s = load_floats<T>(p + ch.c);
+        if (ch.tail) t = p[ch.ct];
+    };
+    const auto go_on = [&](int64_t first, int64_t upto) {
+        for (int64_t b = first; b < upto; b += kAhead) {
             const float *p = part + 2 * b * a.D;
             if (ch.some_whole) {
-                Wide f[kBatch];
+                Wide f[kAhead];
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) f[u] = load_floats<T>(p + (b + u < upto ? 2 * u * a.D : 0) + ch.from);
+                for (int u = 0; u < kAhead; ++u) f[u] = load_floats<T>(p + (b + u < upto ? 2 * u * a.D : 0) + ch.from);
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u)
+                for (int u = 0; u < kAhead; ++u)
                     if (b + u < upto) s += f[u];
             }
             if (ch.some_tail) {
-                float f[kBatch];
+                float f[kAhead];
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) f[u] = p[(b + u < upto ? 2 * u * a.D : 0) + ch.from_tail];
+                for (int u = 0; u < kAhead; ++u) f[u] = p[(b + u < upto ? 2 * u * a.D : 0) + ch.from_tail];
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u)
+                for (int u = 0; u < kAhead; ++u)
                     if (b + u < upto) t += f[u];
             }
         }
-        if (shared) {
-            __syncthreads();  // the one before has been read
+    };
+    if (group < kJoinChunks && counts[group] > 0 && counts[group] <= kMany) {
+        const int64_t chunk = from + group;
+        begin(chunk);
+        go_on(chunk + 1, chunk + 1 + counts[group]);
+        ch.put(G + static_cast<int64_t>(tokens[group]) * a.D, s, t, a.scale, add);
+    }
+    for (int i = 0; i < kJoinChunks; ++i) {
+        const int n = counts[i];
+        if (n <= kMany) continue;
+        const int64_t chunk = from + i, each = (n + kGroups - 1) / kGroups, first = chunk + 1 + group * each;
+        const int64_t end = chunk + 1 + n;
+        s = 0.0f;
+        t = 0.0f;
+        if (group == 0) begin(chunk);
+        go_on(first, first + each < end ? first + each : end);
+        __syncthreads();  // the one before has been read
 #pragma unroll
-            for (int i = 0; i < ch.kPer; ++i) sums[wave][lane][i] = s[i];
-            tails[wave][lane] = t;
-            __syncthreads();
-            if (wave != 0) continue;
-            for (int w = 1; w < kJoinWaves; ++w) {
+        for (int c = 0; c < kPer; ++c) sums[group][lane][c] = s[c];
+        tails[group][lane] = t;
+        __syncthreads();
+        if (group != 0) continue;
+        for (int g = 1; g < kGroups; ++g) {
 #pragma unroll
-                for (int i = 0; i < ch.kPer; ++i) s[i] += sums[w][lane][i];
-                t += tails[w][lane];
-            }
+            for (int c = 0; c < kPer; ++c) s[c] += sums[g][lane][c];
+            t += tails[g][lane];
         }
-        ch.put(G + static_cast<int64_t>(token) * a.D, s, t, a.scale, add);
+        ch.put(G + static_cast<int64_t>(tokens[i]) * a.D, s, t, a.scale, add);
     }
 }
 
@@ -621,13 +655,19 @@ void with_task(int chunk, int width, F &&f) {
         f(integral_constant<int, 64>{}, integral_constant<int, kChunkLong>{});
 }
 
-// Rows of a workgroup of k_embed_few: 8 to 128 KB of G, to fill the card.
+// Rows of a workgroup of k_embed_few: 8 to 128 KB of G, to fill the card, and up
+// to 64, as the tokens among them are added one wave each (192 tokens, bf16: 16 x
+// 30000 x 64 29.8 us so and 34.5 with 512, 26 x 53776 x 77 84.6 and 93.7).
+constexpr int64_t kFewRowsMost = 64, kFewGroupsMost = int64_t(1) << 22;
 int64_t few_rows(int64_t M, int64_t V, int64_t D) {
     int64_t floats = M * V * D / 4096;
     if (floats < 2048) floats = 2048;
     if (floats > kFillFloats) floats = kFillFloats;
-    const int64_t rows = floats / D;
-    return rows < 1 ? 1 : rows;
+    int64_t rows = floats / D;
+    if (rows < 1) rows = 1;
+    if (rows > kFewRowsMost) rows = kFewRowsMost;
+    const int64_t least = ceil_div(M * V, kFewGroupsMost);  // a launch has fewer than 2^32 threads
+    return rows < least ? least : rows;
 }
 
 dqgan_status check(dqgan_plan P, const dqgan_embed_desc *d) {
@@ -734,8 +774,8 @@ dqgan_status dqgan_embed_backward(dqgan_plan P, const dqgan_embed_desc *d, const
             with_index(d->index_type, [&](auto i) {
                 using T = decltype(t);
                 using I = decltype(i);
-                k_embed_few<T, I><<<dim3(static_cast<uint32_t>(ceil_div(a.V, rows)), static_cast<uint32_t>(M)), 64 * kFewWaves, 0, st>>>(
-                    static_cast<const I *>(tok), static_cast<const T *>(dout), a, rows,
+                k_embed_few<T, I><<<static_cast<uint32_t>(M * ceil_div(a.V, rows)), 64 * kFewWaves, 0, st>>>(
+                    static_cast<const I *>(tok), static_cast<const T *>(dout), a, static_cast<uint32_t>(M), rows,
                     slabs_of(a.D, Vec16<T>::kPer), width_of(a.D, Vec16<T>::kPer), G, add != 0);
             });
         });
@@ -780,7 +820,7 @@ dqgan_status dqgan_embed_backward(dqgan_plan P, const dqgan_embed_desc *d, const
                     key[now], at[now], static_cast<const T *>(dout), a, chunks, slabs, width, part, G, add != 0);
             });
             if (chunks > 2)
-                k_embed_join<T, C><<<dim3(static_cast<uint32_t>(ceil_div(chunks, kJoinChunks) * slabs), my), 64 * kJoinWaves, 0,
+                k_embed_join<T, L, C><<<dim3(static_cast<uint32_t>(ceil_div(chunks, kJoinChunks) * slabs), my), 64 * kJoinWaves, 0,
                                      st>>>(key[now], a, chunks, slabs, width, part, G, add != 0);
         });
     });

@@ -162,3 +162,44 @@ def test_tables_beyond_32_bits():
     assert int(torch.count_nonzero(table.any(1))) == 4
     assert bool((G[0, :off] == 7.0).all()) and bool((G[0, off + V * D:] == 7.0).all())
     pl.close()
+
+
+def test_more_rows_than_a_launch_has_workgroups():
+    """A table of 600 million rows of one channel: few tokens, at its ends."""
+    import torch
+    from paper_2010_13359_amd import layers
+    V = 600_000_000
+    print("rows", V, flush=True)
+    plan = ref.plan(V, 1)
+    G = torch.full((1, plan.ld), 7.0, device="cuda")
+    tok = torch.tensor([[0, V - 1, V - 1, 5, V // 2, -1, V]], device="cuda")
+    dout = torch.arange(1.0, 8.0, device="cuda").view(1, 7, 1)
+    layers.embed_backward(plan, tok, dout, G, V, None)
+    assert G[0, [0, V - 1, 5, V // 2, 1]].tolist() == [1.0, 5.0, 4.0, 5.0, 0.0]
+    assert float(G[0, :V].sum(dtype=torch.float64)) == 15.0 and bool((G[0, V:] == 7.0).all())
+    plan.close()
+
+
+@pytest.mark.parametrize("dt", sorted(ref.TYPES))
+@pytest.mark.parametrize("D", [1, 20, 64, 100, 128, 130, 600])
+def test_tokens_of_very_many_places(D, dt):
+    """One token that is all of a worker's places, or all but some at either end,
+    over 64 and 4096 chunks.  Whole numbers, whose sums are exact in 32 bits."""
+    import torch
+    from paper_2010_13359_amd import layers
+    V, N = 9, 140_000 if D < 100 else 40_000
+    gen = torch.Generator().manual_seed(D)
+    tok = torch.full((4, N), 4)
+    tok[1, :70] = 2
+    tok[2, N - 3:] = torch.tensor([8, 5, -1])
+    tok[3] = torch.randint(3, 5, (N,), generator=gen)
+    dout = torch.randint(-8, 9, (4, N, D), generator=gen).to(ref.TYPES[dt])
+    plan = ref.plan(V * D, 4)
+    G = torch.full((4, plan.ld), 3.0, device="cuda")
+    ws = layers.embed_workspace(plan, N, V, D, dout.dtype)
+    layers.embed_backward(plan, tok.cuda(), dout.cuda(), G, V, ws, scale=0.5)
+    for m in range(4):
+        keep = tok[m] >= 0
+        want = torch.zeros((V, D)).index_add_(0, tok[m][keep], dout[m][keep].float()) * 0.5
+        assert torch.equal(G[m, :V * D].view(V, D).cpu(), want), m
+    plan.close()
