@@ -31,7 +31,8 @@
  *    as it was.
  *  - Activations are read to binary32, all sums, maxima and statistics are
  *    binary32 or wider, and each result is rounded to `type` once.  The order
- *    of every sum is fixed by the sizes: equal calls give equal bits.
+ *    of every sum is fixed by the sizes, and for the embedding's gradient by the
+ *    tokens: equal calls give equal bits.
  *  - tokens = 0 is allowed (the activations' pointers may then be NULL).
  *    M * tokens is at most 2^31 - 1.
  */
@@ -68,11 +69,12 @@ typedef struct {
 dqgan_status dqgan_embed_forward(dqgan_plan plan, const dqgan_embed_desc *desc, const void *tok, const float *P,
                                  int64_t ldp, void *out, void *stream);
 
-/* Bytes of dqgan_embed_backward's workspace. */
+/* Bytes of dqgan_embed_backward's workspace (0 for few tokens). */
 dqgan_status dqgan_embed_bytes(dqgan_plan plan, const dqgan_embed_desc *desc, size_t *bytes);
 
 /* G[m][offset + v * width + c] (+)= scale * sum of dout[m][n][c] over the n with
- * tok[m][n] = v, in ascending n; rows of no token are written as 0 (add: left). */
+ * tok[m][n] = v, in parts of consecutive n that are then added in their order; rows
+ * of no token are written as 0 (add: left as they are). */
 dqgan_status dqgan_embed_backward(dqgan_plan plan, const dqgan_embed_desc *desc, const void *tok, const void *dout,
                                   float *G, int32_t add, void *workspace, void *stream);
 
@@ -87,7 +89,8 @@ typedef struct {
 } dqgan_norm_desc;
 
 /* y = (x - mean) * rstd * gamma + beta with the mean and rstd = 1 / sqrt(var + eps)
- * of each row (var: the mean square of x - mean).
+ * of each row (var: the mean square of x - mean, which has to be within binary32;
+ * a row of equal elements needs eps > 0).
  *   x, y [M][tokens][width]; y may be x.
  *   stats [M][tokens][2] fp32 (mean, rstd) or NULL.
  *   P may be NULL if there is neither weight nor bias. */

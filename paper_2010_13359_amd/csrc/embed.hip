@@ -11,12 +11,17 @@
 //                  launch write the table's part of G as 0 meanwhile;
 //   k_embed_merge  joins kFan sorted runs to one, as often as there is more than
 //                  one run: each token counts the smaller ones in the other runs;
-//   k_embed_sum    chunks of kChunk sorted places, one wave per chunk and 1 KB of
-//                  dout's rows.  It writes the rows of the tokens that begin in
-//                  its chunk and end there or in the next.  One that runs on
-//                  leaves a partial sum in each of its chunks, so that a frequent
-//                  token is as much work as a rare one;
+//   k_embed_sum    chunks of 8 or 32 sorted places, one wave per chunk and 1 KB of
+//                  dout's rows, or several chunks per wave where the rows are
+//                  narrow.  It writes the rows of the tokens that begin in its
+//                  chunk and end there or in the next.  One that runs on leaves a
+//                  partial sum in each of its chunks, so that a frequent token is
+//                  as much work as a rare one;
 //   k_embed_join   sums those.
+// No sum uses atomics: its order goes by the tokens alone, and the same call gives
+// the same bits.  All of it is bound by memory: for 8 x 4096 tokens, tables of 32000 x
+// 1024 and bf16, the launch that writes 1.05 GB of zeros beside the sort takes 164 us
+// (6.4 TB/s, a plain fill 6.9), the sums 44 and the join 5.
 #include "layers.hpp"
 
 namespace dq {
@@ -34,9 +39,10 @@ struct EmbedArgs {
 };
 
 // 1 << shift consecutive threads per token, four channels each, forward_rows
-// tokens at a time: their rows are asked for before the first is used (one at a
-// time: 74.6 us where four take 47.3).  A padded place reads
-// the table's first row and writes 0.
+// tokens at a time: their rows are asked for before the first is used (8 x 8192
+// tokens, rows of 1024, to bf16: 47 us, one at a time 74.6; 402 MB at most, if no
+// token came twice, are 8.5 TB/s, as frequent rows stay in the caches).  A padded
+// place reads the table's first row and writes 0.
 template <typename T>
 constexpr int forward_rows = sizeof(T) == 4 ? 2 : 4;
 template <typename T, typename I, bool STREAM>
@@ -107,6 +113,8 @@ __device__ __forceinline__ uint32_t key_of(const I *tok, int64_t i, int64_t V) {
 // Stable sort of one run by digits from the lowest up, in registers and LDS.  A
 // wave owns 256 consecutive places and, of the counters [digit][wave], its own
 // column; a lane finds the lanes of its wave with its digit by one ballot a bit.
+// 4096 tokens of 15 bits, two passes: 8.5 us, of 16 runs at a time 11.3; each
+// pass is five waits for the whole workgroup.
 template <typename I>
 __device__ void sort_run(const I *tok, int64_t begin, int64_t N, int64_t V, int bits, int passes, uint32_t *key,
                          uint32_t *at) {
