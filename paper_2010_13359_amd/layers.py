@@ -93,11 +93,16 @@ def _desc(plan, cls, fn, *fields):
     return hit
 
 
-def _shape(plan, t, name, dims):
-    """Shape of the tensor that says what sizes a call has."""
-    if not isinstance(t, torch.Tensor) or t.dim() != dims or t.shape[0] != plan.M:
-        raise ValueError("%s: expected a tensor of [%d][tokens]%s" % (name, plan.M, "[width]" if dims == 3 else ""))
-    return t.shape
+def _sizes(plan, t, name):
+    """Device pointer, shape and dtype of the tensor that says what sizes a call has."""
+    if isinstance(t, torch.Tensor):
+        shape = t.shape
+        if len(shape) == 3 and shape[0] == plan.M:
+            dtype = t.dtype
+            if dtype in TYPES and t.get_device() == plan.device and t.is_contiguous():
+                return t.data_ptr() or None, shape, dtype
+            _ptr(t, name, 0, TYPES, plan.device)
+    raise ValueError("%s: expected a tensor of [%d][tokens][width]" % (name, plan.M))
 
 
 def _like(plan, t, name, shape, dtypes):
@@ -117,6 +122,10 @@ def _params(plan, P):
     one vector of ld that all workers read."""
     if P is None:
         return None, plan.ld
+    # the usual case by the fewest attribute reads; what fails here is named below
+    if (isinstance(P, torch.Tensor) and P.dtype == torch.float32 and P.dim() == 2 and P.get_device() == plan.device
+            and P.is_contiguous() and P.nbytes >= 4 * plan.M * plan.ld):
+        return P.data_ptr(), plan.ld
     if isinstance(P, torch.Tensor) and P.dim() == 1 and plan.M > 1:
         return plan._vec(P, "P"), 0
     return plan._mat(P, "P"), plan.ld
@@ -146,11 +155,12 @@ def _new(plan, n):
 
 
 def _embed(plan, tokens, x, name, vocab, offset, scale):
-    """Descriptor, workspace and token pointer of a call whose activations are x."""
-    shape = _shape(plan, x, name, 3)
+    """Descriptor, workspace, pointers of the tokens and of the activations x."""
+    at, shape, dtype = _sizes(plan, x, name)
     tok = _like(plan, tokens, "tokens", shape[:2], INDEX_TYPES)
-    return _desc(plan, EmbedDesc, "dqgan_embed_bytes", offset, vocab, shape[2], shape[1], scale, _type(x.dtype, name),
-                 INDEX_TYPES.get(getattr(tokens, "dtype", None), 0), 0) + (tok,)
+    d, need = _desc(plan, EmbedDesc, "dqgan_embed_bytes", offset, vocab, shape[2], shape[1], scale, TYPES[dtype],
+                    0 if tokens is None else INDEX_TYPES[tokens.dtype], 0)
+    return d, need, tok, at
 
 
 def embed_forward(plan, tokens, P, out, vocab, offset=0, scale=1.0, stream=None):
@@ -158,11 +168,9 @@ def embed_forward(plan, tokens, P, out, vocab, offset=0, scale=1.0, stream=None)
     `offset` of its row of P ([vocab][width]); 0 where the token is below 0 or
     at or beyond vocab.  tokens int32 or int64 [M][tokens]; P [M][ld], or [ld]
     for all workers; out [M][tokens][width]."""
-    d, _, tok = _embed(plan, tokens, out, "out", vocab, offset, scale)
+    d, _, tok, to = _embed(plan, tokens, out, "out", vocab, offset, scale)
     p, ldp = _params(plan, P)
-    _check("dqgan_embed_forward", load().dqgan_embed_forward(plan.handle, d, tok, p, ldp,
-                                                             _like(plan, out, "out", out.shape, TYPES),
-                                                             _on(plan, stream)))
+    _check("dqgan_embed_forward", load().dqgan_embed_forward(plan.handle, d, tok, p, ldp, to, _on(plan, stream)))
 
 
 def embed_workspace(plan, tokens, vocab, width, dtype, index_dtype=torch.int64, offset=0):
@@ -175,10 +183,8 @@ def embed_backward(plan, tokens, dout, G, vocab, workspace, offset=0, scale=1.0,
     """The table's part of G [M][ld]: row v is scale * the sum of dout over the
     tokens that are v, 0 for those that do not occur; with `add` the sums are
     added to what is there."""
-    d, need, tok = _embed(plan, tokens, dout, "dout", vocab, offset, scale)
-    _check("dqgan_embed_backward", load().dqgan_embed_backward(plan.handle, d, tok,
-                                                               _like(plan, dout, "dout", dout.shape, TYPES),
-                                                               plan._mat(G, "G"), int(add),
+    d, need, tok, at = _embed(plan, tokens, dout, "dout", vocab, offset, scale)
+    _check("dqgan_embed_backward", load().dqgan_embed_backward(plan.handle, d, tok, at, plan._mat(G, "G"), int(add),
                                                                _workspace(plan, workspace, need), _on(plan, stream)))
 
 
@@ -186,9 +192,9 @@ def embed_backward(plan, tokens, dout, G, vocab, workspace, offset=0, scale=1.0,
 # layer norm
 
 
-def _norm(plan, tokens, width, dtype, name, gamma, beta, eps):
+def _norm(plan, tokens, width, type, gamma, beta, eps):
     return _desc(plan, NormDesc, "dqgan_norm_bytes", -1 if gamma is None else gamma, -1 if beta is None else beta, width,
-                 tokens, eps, _type(dtype, name), 0)
+                 tokens, eps, type, 0)
 
 
 def norm_forward(plan, x, P, y, stats=None, gamma=0, beta=None, eps=1e-5, stream=None):
@@ -196,32 +202,29 @@ def norm_forward(plan, x, P, y, stats=None, gamma=0, beta=None, eps=1e-5, stream
     bias at `gamma` and `beta` of each worker's row of P (None: without).
     stats [M][tokens][2] float32 takes mean and rstd for norm_backward; y may
     be x."""
-    shape = _shape(plan, x, "x", 3)
-    d, _ = _norm(plan, shape[1], shape[2], x.dtype, "x", gamma, beta, eps)
+    at, shape, dtype = _sizes(plan, x, "x")
+    d, _ = _norm(plan, shape[1], shape[2], TYPES[dtype], gamma, beta, eps)
     p, ldp = _params(plan, P)
-    same = (x.dtype,)
     _check("dqgan_norm_forward",
-           load().dqgan_norm_forward(plan.handle, d, _like(plan, x, "x", shape, same), p, ldp,
-                                     _like(plan, y, "y", shape, same),
+           load().dqgan_norm_forward(plan.handle, d, at, p, ldp, _like(plan, y, "y", shape, (dtype,)),
                                      _like(plan, stats, "stats", (shape[0], shape[1], 2), F32), _on(plan, stream)))
 
 
 def norm_workspace(plan, tokens, width, dtype, gamma=0, beta=None):
     """A workspace for norm_backward of these sizes (None if it needs none)."""
-    return _new(plan, _norm(plan, tokens, width, dtype, "dtype", gamma, beta, 0.0)[1])
+    return _new(plan, _norm(plan, tokens, width, _type(dtype, "dtype"), gamma, beta, 0.0)[1])
 
 
 def norm_backward(plan, x, dy, P, stats, dx, G, workspace, gamma=0, beta=None, add=False, stream=None):
     """dx (None: not wanted; it may be dy), and the sums over a worker's tokens
     of dy * (x - mean) * rstd and of dy into its row of G at `gamma` and
     `beta`; with `add` added to what is there."""
-    shape = _shape(plan, x, "x", 3)
-    d, need = _norm(plan, shape[1], shape[2], x.dtype, "x", gamma, beta, 0.0)
+    at, shape, dtype = _sizes(plan, x, "x")
+    d, need = _norm(plan, shape[1], shape[2], TYPES[dtype], gamma, beta, 0.0)
     p, ldp = _params(plan, P)
-    same = (x.dtype,)
+    same = (dtype,)
     _check("dqgan_norm_backward",
-           load().dqgan_norm_backward(plan.handle, d, _like(plan, x, "x", shape, same),
-                                      _like(plan, dy, "dy", shape, same), p, ldp,
+           load().dqgan_norm_backward(plan.handle, d, at, _like(plan, dy, "dy", shape, same), p, ldp,
                                       _like(plan, stats, "stats", (shape[0], shape[1], 2), F32),
                                       _like(plan, dx, "dx", shape, same), plan._mat(G, "G"), int(add),
                                       _workspace(plan, workspace, need), _on(plan, stream)))
@@ -234,14 +237,14 @@ def norm_backward(plan, x, dy, P, stats, dx, G, workspace, gamma=0, beta=None, a
 def _distill(plan, z, val, idx, weight, vocab, temperature):
     """Descriptor, workspace, the pointers that every form of the loss takes,
     and [M][tokens]."""
-    shape = _shape(plan, z, "z", 3)
+    at, shape, dtype = _sizes(plan, z, "z")
     rows = shape[:2]
     if not isinstance(val, torch.Tensor) or val.dim() != 3:
         raise ValueError("val: expected a tensor of [%d][%d][k]" % rows)
     sent = (rows[0], rows[1], val.shape[2])
     d, need = _desc(plan, DistillDesc, "dqgan_distill_bytes", shape[2] if vocab is None else vocab, shape[2], rows[1],
-                    sent[2], temperature, _type(z.dtype, "z"), 0)
-    return d, need, (_like(plan, z, "z", shape, TYPES), _like(plan, val, "val", sent, F32),
+                    sent[2], temperature, TYPES[dtype], 0)
+    return d, need, (at, _like(plan, val, "val", sent, F32),
                      _like(plan, idx, "idx", sent, U32), _like(plan, weight, "weight", rows, F32)), rows
 
 
