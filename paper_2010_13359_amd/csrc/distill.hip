@@ -230,6 +230,11 @@ __device__ void clear(T *to, int64_t begin, int64_t end) {
     for (int64_t c = begin + 8 * threadIdx.x; c < end; c += 8 * 64 * W) store8(to + c, end - c, f32x8(0.0f));
 }
 
+// Vectors per lane of a 16-wave workgroup that leave room for a second one on its
+// CU, at 64 registers a lane (loss and gradient of 4096 x 80000 bf16 logits 233 us,
+// 333 with one of 16 vectors; the loss 131 and 228).
+constexpr int kTwoVectors = 12;
+
 // One workgroup per token, whose logits stay in registers between the
 // statistics and the gradient, so that z is read once: largest logit, sum of the
 // exponentials, then dz from the same registers; the message's entries are written
@@ -240,7 +245,7 @@ __device__ void clear(T *to, int64_t begin, int64_t end) {
 // first only reads, then computes, then only writes, with three others on its CU;
 // one workgroup a CU that asks for the next row meanwhile took 875 us in place of 830.
 template <typename T, int W, int NV, bool LOSS, bool GRAD, bool STREAM>
-__global__ __launch_bounds__(64 * W) void k_distill_row(const T *z, DistillArgs a, float *loss, float *stats, T *dz) {
+__global__ __launch_bounds__(64 * W, NV == kTwoVectors ? 8 : 1) void k_distill_row(const T *z, DistillArgs a, float *loss, float *stats, T *dz) {
     constexpr bool FINE = sizeof(T) == 4;
     constexpr int kPer = Vec16<T>::kPer;
     __shared__ Message s;
@@ -386,6 +391,7 @@ __global__ __launch_bounds__(256) void k_distill_slice(const T *z, DistillArgs a
 
 // f(W, NV) with the smallest row shape that holds `bytes` (up to kRowMost).  A lane
 // keeps up to 64 registers of logits.
+constexpr int64_t kRowMost = 262144, kTwoRows = 16 * 64 * 16 * kTwoVectors, kRowFewer = 131072, kFewRows = 128;
 template <typename F>
 void with_shape(int64_t bytes, F &&f) {
     using std::integral_constant;
@@ -401,19 +407,24 @@ void with_shape(int64_t bytes, F &&f) {
         f(integral_constant<int, 4>{}, integral_constant<int, 16>{});
     else if (bytes <= 131072)
         f(integral_constant<int, 8>{}, integral_constant<int, 16>{});
+    else if (bytes <= kTwoRows)
+        f(integral_constant<int, 16>{}, integral_constant<int, kTwoVectors>{});
     else
         f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
 }
 
-// Rows are shared out in slices where a row does not fit a workgroup's
-// registers, and where it takes a CU's whole and there are so few that most CUs
-// would have none: loss and gradient of 64 rows of 128000 bf16 logits 15.3 us in
-// slices and 21.3 by rows, of 256 rows 43 and 35.
-constexpr int64_t kRowMost = 262144, kRowFewer = 131072, kFewRows = 96;
+// Rows are shared out in slices
+//  - where a row does not fit a workgroup's registers;
+//  - where it takes half a CU or more and there are so few that most CUs would have
+//    none: loss and gradient of 64 rows of 128000 bf16 logits 15 us in slices and
+//    21 by rows, of 128 rows of 80000 16 and 18, of 256 26 and 22.
+// The rule does not ask whether the gradient is wanted too, so that the loss has the
+// same bits with it and without (slices would be faster for the loss alone of 4096
+// rows of 128000: 197 us and 250).
 bool split(int64_t rows, int64_t bytes) { return bytes > kRowMost || (bytes > kRowFewer && rows <= kFewRows); }
 int64_t slices_of(int64_t bytes) { return ceil_div(bytes, 64 * 4 * kSliceVectors * 16); }
 
-// Whether long rows (16 vectors a lane) pass by the caches: loss and gradient of
+// Whether long rows (12 or 16 vectors a lane) pass by the caches: loss and gradient of
 // 32000 bf16 logits, read and written, of 33 MB in all 11.5 us so and 11.9
 // with ordinary accesses, of 132 MB 28.6 / 33.1, 526 MB 102 / 115; of 128000
 // logits 8 MB 20.7 / 18.8, 1050 MB 221 / 236, 2500 MB 580 / 563.  Entries are
@@ -494,8 +505,8 @@ dqgan_status run(dqgan_plan P, const dqgan_distill_desc *d, const void *z, const
             float *l = loss ? loss + r : loss, *x = stats ? stats + 2 * r : stats;
             with_shape(bytes, [&](auto w, auto nv) {
                 constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-                if (GRAD && NV == 16 && streams(rows, bytes, d->k))
-                    k_distill_row<T, W, NV, LOSS, GRAD, GRAD && NV == 16><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
+                if (GRAD && NV >= kTwoVectors && streams(rows, bytes, d->k))
+                    k_distill_row<T, W, NV, LOSS, GRAD, GRAD && NV >= kTwoVectors><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
                 else
                     k_distill_row<T, W, NV, LOSS, GRAD, false><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
             });

@@ -80,6 +80,15 @@ def test_loss_and_gradient(shape, dt):
         pl.close()
 
 
+@pytest.mark.parametrize("dt,V", [("bf16", 65537), ("bf16", 98304), ("f16", 98305), ("bf16", 131072), ("f32", 40001),
+                                  ("f32", 49152), ("f32", 49153), ("f32", 65533)])
+def test_long_rows_of_many_tokens(dt, V):
+    """Rows of half a CU's registers and more, enough of them for a workgroup each."""
+    pl, z, val, idx, weight = _setup((1, 131, V, 1, 9), dt, seed=V)
+    _compare(z, val, idx, weight, V, 1.0, _run(pl, z, val, idx, weight, V, 1.0))
+    pl.close()
+
+
 @pytest.mark.parametrize("dt", sorted(ref.TYPES))
 @pytest.mark.parametrize("V", [40, 5000, 70001, 140000])
 def test_tokens_that_take_no_part(V, dt):
