@@ -155,9 +155,11 @@ __device__ float entry_gradient(const DistillArgs &a, const Message &s, int have
     return (exp_of<FINE>(a, s.z[j], x.largest) / x.total - sum) * coef;
 }
 
-// NV vectors of 16 bytes per lane of a row's columns [0, V), and the last V % kPer
-// columns one each in the first lanes.  Vectors beyond the row are -inf.
-template <typename T, int W, int NV, bool STREAM>
+// NV vectors of 16 bytes per lane of a row's columns [0, V) in registers, NL more in
+// LDS (`held`, kHeld of all lanes together, each used by its own lane only), and the
+// last V % kPer columns one each in the first lanes.  Vectors beyond the row are -inf.
+constexpr int kHeld = 4032;
+template <typename T, int W, int NV, int NL, bool STREAM>
 struct Logits {
     typedef typename Vec16<T>::type Raw;
     typedef typename Vec16<T>::packed Packed;
@@ -167,58 +169,91 @@ struct Logits {
     Raw raw[NV];
     float last;
 
-    __device__ __forceinline__ void load(const T *from, int vectors, int rest) {
+    static __device__ __forceinline__ int at(int v) { return static_cast<int>(threadIdx.x) + 64 * W * v; }
+    template <int FROM, int UPTO>
+    __device__ __forceinline__ void load_part(const T *from, int vectors, Raw *to) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int q = threadIdx.x + 64 * W * v;
-            if (q < vectors) {
-                const Packed *p = reinterpret_cast<const Packed *>(from) + q;
-                raw[v] = STREAM ? __builtin_nontemporal_load(p) : *p;
+        for (int v = FROM; v < UPTO; ++v) {
+            if (at(v) < vectors) {
+                const Packed *p = reinterpret_cast<const Packed *>(from) + at(v);
+                to[v - FROM] = STREAM ? __builtin_nontemporal_load(p) : *p;
             } else {
-                raw[v] = static_cast<T>(kNone);
+                to[v - FROM] = static_cast<T>(kNone);
             }
+        }
+    }
+    __device__ __forceinline__ void load(const T *from, int vectors, int rest, Raw *held) {
+        if constexpr (NL == 0) {
+            load_part<0, NV>(from, vectors, raw);
+        } else {
+            // as many as fit at a time: the first ones go to LDS as soon as they are here
+            Raw first[NL];
+            load_part<NV, NV + NL>(from, vectors, first);
+            load_part<0, NV - NL>(from, vectors, raw);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int v = 0; v < NL; ++v)
+                if (at(NV + v) < vectors) held[at(v)] = first[v];
+            __builtin_amdgcn_sched_barrier(0);
+            load_part<NV - NL, NV>(from, vectors, raw + NV - NL);
         }
         last = static_cast<int>(threadIdx.x) < rest ? static_cast<float>(from[kPer * vectors + threadIdx.x]) : kNone;
     }
-    __device__ __forceinline__ float largest() const {
-        float top = last;
+    __device__ __forceinline__ static float most(Raw r, float top) {
+        const Wide f = __builtin_convertvector(r, Wide);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const Wide f = __builtin_convertvector(raw[v], Wide);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) top = fmaxf(top, f[i]);
-        }
+        for (int i = 0; i < kPer; ++i) top = fmaxf(top, f[i]);
         return top;
     }
-    __device__ __forceinline__ float sum(const DistillArgs &a, float ref) {
+    __device__ __forceinline__ float largest(int vectors, const Raw *held) const {
+        float top = last;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) top = most(raw[v], top);
+#pragma unroll
+        for (int v = 0; v < NL; ++v)
+            if (at(NV + v) < vectors) top = most(held[at(v)], top);
+        return top;
+    }
+    __device__ __forceinline__ static float add(const DistillArgs &a, Raw r, float ref, float sum) {
+        const Wide f = __builtin_convertvector(r, Wide);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) sum += exp_of<FINE>(a, f[i], ref);
+        return sum;
+    }
+    __device__ __forceinline__ float sum(const DistillArgs &a, float ref, int vectors, const Raw *held) {
         float sum = exp_of<FINE>(a, last, ref);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             forget(raw[v]);
-            const Wide f = __builtin_convertvector(raw[v], Wide);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) sum += exp_of<FINE>(a, f[i], ref);
+            sum = add(a, raw[v], ref, sum);
         }
+#pragma unroll
+        for (int v = 0; v < NL; ++v)
+            if (at(NV + v) < vectors) sum = add(a, held[at(v)], ref, sum);
         return sum;
     }
     // s * over
-    __device__ __forceinline__ void gradient(const DistillArgs &a, float largest, float over, T *to, int vectors, int rest) {
+    __device__ __forceinline__ static void put(const DistillArgs &a, Raw r, float largest, float over, T *to, int q) {
+        Wide f = __builtin_convertvector(r, Wide);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) f[i] = exp_of<FINE>(a, f[i], largest) * over;
+        Packed *p = reinterpret_cast<Packed *>(to) + q;
+        r = __builtin_convertvector(f, Raw);
+        if (STREAM)
+            __builtin_nontemporal_store(r, p);
+        else
+            *p = r;
+    }
+    __device__ __forceinline__ void gradient(const DistillArgs &a, float largest, float over, T *to, int vectors, int rest,
+                                             const Raw *held) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int q = threadIdx.x + 64 * W * v;
             forget(raw[v]);
-            Wide f = __builtin_convertvector(raw[v], Wide);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) f[i] = exp_of<FINE>(a, f[i], largest) * over;
-            if (q < vectors) {
-                Packed *p = reinterpret_cast<Packed *>(to) + q;
-                const Raw r = __builtin_convertvector(f, Raw);
-                if (STREAM)
-                    __builtin_nontemporal_store(r, p);
-                else
-                    *p = r;
-            }
+            if (at(v) < vectors) put(a, raw[v], largest, over, to, at(v));
         }
+#pragma unroll
+        for (int v = 0; v < NL; ++v)
+            if (at(NV + v) < vectors) put(a, held[at(v)], largest, over, to, at(NV + v));
         if (static_cast<int>(threadIdx.x) < rest)
             to[kPer * vectors + threadIdx.x] = static_cast<T>(exp_of<FINE>(a, last, largest) * over);
     }
@@ -232,19 +267,22 @@ __device__ void clear(T *to, int64_t begin, int64_t end) {
 
 // Vectors per lane of a 16-wave workgroup that leave room for a second one on its
 // CU, at 64 registers a lane (loss and gradient of 4096 x 80000 bf16 logits 233 us,
-// 333 with one of 16 vectors; the loss 131 and 228).
-constexpr int kTwoVectors = 12;
+// 333 with one of 16 vectors; the loss 130 and 228), and how many more fit half a
+// CU's LDS beside the message (4096 x 128000: 380 us, 429 with one workgroup of 16
+// vectors; the loss 182 and 250).
+constexpr int kTwoVectors = 12, kTwoHeld = 4;
 
 // One workgroup per token, whose logits stay in registers between the
 // statistics and the gradient, so that z is read once: largest logit, sum of the
 // exponentials, then dz from the same registers; the message's entries are written
 // over it last.  LOSS: the statistics and the loss; GRAD: dz, from the statistics
-// just made or (LOSS not) from `stats`.  Loss and gradient of 4096 x 32000 bf16
-// logits (528 MB) 105 us, 5.0 TB/s; of 8192 x 128000 (4.2 GB) 845, 5.0; the gradient
-// of 3108 x 30011 f16 72 us.  What keeps it from a copy's 6.1 is that a workgroup
-// first only reads, then computes, then only writes, with three others on its CU;
-// one workgroup a CU that asks for the next row meanwhile took 875 us in place of 830.
-template <typename T, int W, int NV, bool LOSS, bool GRAD, bool STREAM>
+// just made or (LOSS not) from `stats`.  Bound by memory: loss and gradient of 4096
+// x 32000 bf16 logits (528 MB) 102 us, 5.2 TB/s; of 8192 x 128000 (4.2 GB) 823, 5.1;
+// the gradient of 3108 x 30011 f16 72 us.  What keeps it from a copy's 6.1 is that a
+// workgroup first only reads, then computes, then only writes, and what overlaps is
+// the others on its CU; one workgroup a CU that asks for the next row meanwhile was
+// slower than two that do not.
+template <typename T, int W, int NV, int NL, bool LOSS, bool GRAD, bool STREAM>
 __global__ __launch_bounds__(64 * W, NV == kTwoVectors ? 8 : 1) void k_distill_row(const T *z, DistillArgs a, float *loss, float *stats, T *dz) {
     constexpr bool FINE = sizeof(T) == 4;
     constexpr int kPer = Vec16<T>::kPer;
@@ -257,15 +295,16 @@ __global__ __launch_bounds__(64 * W, NV == kTwoVectors ? 8 : 1) void k_distill_r
     const int vectors = static_cast<int>(a.V / kPer), rest = static_cast<int>(a.V % kPer);
     int have = 0;
     Softmax x{0.0f, 0.0f};
-    Logits<T, W, NV, STREAM> l;
+    Logits<T, W, NV, NL, STREAM> l;
+    __shared__ typename Vec16<T>::type held[NL > 0 ? kHeld : 1];
     if (weight != 0.0f) {
-        l.load(from, vectors, rest);
+        l.load(from, vectors, rest, held);
         have = teacher<T, W, GRAD>(a, row, from, nullptr, 0, a.V, s);
     }
     if (have != 0) {
         if (LOSS) {
-            x.largest = group_max<W>(l.largest(), s.slots[2]);
-            x.total = group_sum<W>(l.sum(a, reference(x.largest)), s.slots[3]);
+            x.largest = group_max<W>(l.largest(vectors, held), s.slots[2]);
+            x.total = group_sum<W>(l.sum(a, reference(x.largest), vectors, held), s.slots[3]);
             if (x.largest == kNone && x.total == 0.0f) have = 0;
         } else {
             x.largest = stats[2 * row];
@@ -290,7 +329,7 @@ __global__ __launch_bounds__(64 * W, NV == kTwoVectors ? 8 : 1) void k_distill_r
             return;
         }
         const float coef = weight * a.T, over = coef / x.total;
-        l.gradient(a, x.largest, over, to, vectors, rest);
+        l.gradient(a, x.largest, over, to, vectors, rest, held);
         clear<T, W>(to, a.V, a.ld);
         __syncthreads();
         for (int j = tid; j < a.k; j += 64 * W)
@@ -313,14 +352,14 @@ __global__ __launch_bounds__(256) void k_distill_part(const T *z, DistillArgs a,
     if (a.weight && a.weight[row] == 0.0f) return;
     const int64_t n = a.V - begin < kSlice<T> ? a.V - begin : kSlice<T>;
     const T *from = z + row * a.ld;
-    Logits<T, 4, kSliceVectors, false> l;
-    l.load(from + begin, static_cast<int>(n / Vec16<T>::kPer), static_cast<int>(n % Vec16<T>::kPer));
+    Logits<T, 4, kSliceVectors, 0, false> l;
+    l.load(from + begin, static_cast<int>(n / Vec16<T>::kPer), static_cast<int>(n % Vec16<T>::kPer), nullptr);
     for (int64_t j = blockIdx.x * 256 + threadIdx.x; j < a.k; j += 256 * gridDim.x) {
         const uint32_t i = a.idx[row * a.k + j];
         if (i < a.V) gathered[row * a.k + j] = static_cast<float>(from[i]);
     }
-    const float largest = group_max<4>(l.largest(), slots[0]);
-    const float total = group_sum<4>(l.sum(a, reference(largest)), slots[1]);
+    const float largest = group_max<4>(l.largest(0, nullptr), slots[0]);
+    const float total = group_sum<4>(l.sum(a, reference(largest), 0, nullptr), slots[1]);
     if (threadIdx.x == 0) part[row * gridDim.x + blockIdx.x] = Softmax{largest, total};
 }
 
@@ -340,9 +379,9 @@ __global__ __launch_bounds__(256) void k_distill_slice(const T *z, DistillArgs a
     const float weight = a.weight ? a.weight[row] : 1.0f;
     int have = 0;
     Softmax x{0.0f, 0.0f};
-    Logits<T, 4, kSliceVectors, false> l;
+    Logits<T, 4, kSliceVectors, 0, false> l;
     if (weight != 0.0f) {
-        if (GRAD) l.load(from + begin, vectors, rest);
+        if (GRAD) l.load(from + begin, vectors, rest, nullptr);
         have = teacher<T, 4, GRAD>(a, row, from, LOSS ? gathered + row * a.k : nullptr, begin, begin + n, s);
     }
     if (have != 0) {
@@ -379,7 +418,7 @@ __global__ __launch_bounds__(256) void k_distill_slice(const T *z, DistillArgs a
             return;
         }
         const float coef = weight * a.T, over = coef / x.total;
-        l.gradient(a, x.largest, over, to + begin, vectors, rest);
+        l.gradient(a, x.largest, over, to + begin, vectors, rest, nullptr);
         __syncthreads();
         for (int j = tid; j < a.k; j += 256) {
             const uint32_t i = s.idx[j];
@@ -389,28 +428,29 @@ __global__ __launch_bounds__(256) void k_distill_slice(const T *z, DistillArgs a
     }
 }
 
-// f(W, NV) with the smallest row shape that holds `bytes` (up to kRowMost).  A lane
-// keeps up to 64 registers of logits.
-constexpr int64_t kRowMost = 262144, kTwoRows = 16 * 64 * 16 * kTwoVectors, kRowFewer = 131072, kFewRows = 128;
+// f(W, NV, NL) with the smallest row shape that holds `bytes` (up to kRowMost).  A
+// lane keeps up to 64 registers of logits.
+constexpr int64_t kTwoRows = 16 * 64 * 16 * kTwoVectors, kRowMost = kTwoRows + 16 * kHeld, kRowFewer = 131072, kFewRows = 128;
+template <int N>
+using Int = std::integral_constant<int, N>;
 template <typename F>
 void with_shape(int64_t bytes, F &&f) {
-    using std::integral_constant;
     if (bytes <= 4096)
-        f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+        f(Int<4>{}, Int<1>{}, Int<0>{});
     else if (bytes <= 8192)
-        f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+        f(Int<4>{}, Int<2>{}, Int<0>{});
     else if (bytes <= 16384)
-        f(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+        f(Int<4>{}, Int<4>{}, Int<0>{});
     else if (bytes <= 32768)
-        f(integral_constant<int, 4>{}, integral_constant<int, 8>{});
+        f(Int<4>{}, Int<8>{}, Int<0>{});
     else if (bytes <= 65536)
-        f(integral_constant<int, 4>{}, integral_constant<int, 16>{});
+        f(Int<4>{}, Int<16>{}, Int<0>{});
     else if (bytes <= 131072)
-        f(integral_constant<int, 8>{}, integral_constant<int, 16>{});
+        f(Int<8>{}, Int<16>{}, Int<0>{});
     else if (bytes <= kTwoRows)
-        f(integral_constant<int, 16>{}, integral_constant<int, kTwoVectors>{});
+        f(Int<16>{}, Int<kTwoVectors>{}, Int<0>{});
     else
-        f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+        f(Int<16>{}, Int<kTwoVectors>{}, Int<kTwoHeld>{});
 }
 
 // Rows are shared out in slices
@@ -424,17 +464,19 @@ void with_shape(int64_t bytes, F &&f) {
 bool split(int64_t rows, int64_t bytes) { return bytes > kRowMost || (bytes > kRowFewer && rows <= kFewRows); }
 int64_t slices_of(int64_t bytes) { return ceil_div(bytes, 64 * 4 * kSliceVectors * 16); }
 
-// Whether long rows (12 or 16 vectors a lane) pass by the caches: loss and gradient of
-// 32000 bf16 logits, read and written, of 33 MB in all 11.5 us so and 11.9
-// with ordinary accesses, of 132 MB 28.6 / 33.1, 526 MB 102 / 115; of 128000
-// logits 8 MB 20.7 / 18.8, 1050 MB 221 / 236, 2500 MB 580 / 563.  Entries are
-// written into the row once more: not if there are as many as lines of 128 bytes
-// (526 MB, 256 entries 117 / 137, 1024 233 / 170).
+// Whether long rows (12 or 16 vectors a lane) pass by the caches: loss and gradient
+// of 60 MB of bf16 logits, read and written, the same; of 120 MB, rows of 32000 29.8
+// us so and 35.6 not, of 128000 31.5 and 37.3; 1 GB 195 / 213 and 201 / 218.  Beyond,
+// rows of more than 64 KB that begin at lines of 128 bytes gain (128000: 2 GB 373 /
+// 399, 4 GB 751 / 764), others lose (98000: 2 GB 420 / 413, 4 GB 844 / 797; 32000: 2 GB
+// 416 / 411).  Entries are written into the row once more: not if there are as
+// many as lines (526 MB of 32000, 256 entries 117 / 137, 1024 233 / 170).
 constexpr double kStreamFrom = 64e6, kStreamUpTo = 1.4e9;
-bool streams(int64_t rows, int64_t bytes, int k) {
-    if (k > bytes / 128) return false;
+bool streams(int64_t rows, const dqgan_distill_desc *d, int64_t bytes) {
+    if (d->k > bytes / 128) return false;
+    const bool lines = bytes > 65536 && d->ld * (bytes / d->vocab) % 128 == 0;
     const double total = 2.0 * static_cast<double>(rows) * static_cast<double>(bytes);
-    return total >= kStreamFrom && total <= kStreamUpTo;
+    return total >= kStreamFrom && (lines || total <= kStreamUpTo);
 }
 
 dqgan_status check(dqgan_plan P, const dqgan_distill_desc *d) {
@@ -503,12 +545,12 @@ dqgan_status run(dqgan_plan P, const dqgan_distill_desc *d, const void *z, const
             const T *from = static_cast<const T *>(z) + r * a.ld;
             T *to = static_cast<T *>(dz) + (GRAD ? r * a.ld : 0);
             float *l = loss ? loss + r : loss, *x = stats ? stats + 2 * r : stats;
-            with_shape(bytes, [&](auto w, auto nv) {
-                constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-                if (GRAD && NV >= kTwoVectors && streams(rows, bytes, d->k))
-                    k_distill_row<T, W, NV, LOSS, GRAD, GRAD && NV >= kTwoVectors><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
+            with_shape(bytes, [&](auto w, auto nv, auto nl) {
+                constexpr int W = decltype(w)::value, NV = decltype(nv)::value, NL = decltype(nl)::value;
+                if (GRAD && NV >= kTwoVectors && streams(rows, d, bytes))
+                    k_distill_row<T, W, NV, NL, LOSS, GRAD, GRAD && NV >= kTwoVectors><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
                 else
-                    k_distill_row<T, W, NV, LOSS, GRAD, false><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
+                    k_distill_row<T, W, NV, NL, LOSS, GRAD, false><<<n, 64 * W, 0, st>>>(from, b, l, x, to);
             });
         });
     }
