@@ -97,7 +97,8 @@ typedef struct {
 dqgan_status dqgan_norm_forward(dqgan_plan plan, const dqgan_norm_desc *desc, const void *x, const float *P,
                                 int64_t ldp, void *y, float *stats, void *stream);
 
-/* Bytes of dqgan_norm_backward's workspace (0 if there is neither weight nor bias). */
+/* Bytes of dqgan_norm_backward's workspace (0 for few tokens, and if there is neither
+ * weight nor bias). */
 dqgan_status dqgan_norm_bytes(dqgan_plan plan, const dqgan_norm_desc *desc, size_t *bytes);
 
 /* With xh = (x - mean) * rstd and u = dy * gamma:

@@ -191,16 +191,24 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const T *x, NormArgs a, 
     }
 }
 
-// One workgroup takes every gridDim.x-th group of rows of its worker, keeps
-// its columns' sums of dy and dy * xh in registers meanwhile and leaves them in
-// part[m][blockIdx.x][2][D]: x and dy are read once for all three results.  8 x
+// Where the columns' sums go: to part[m][share][2][D], or, of one workgroup per
+// worker, to G.  Neither: not wanted.
+struct Sums {
+    float *part, *G;
+    int64_t ld;
+    bool add;
+};
+
+// One workgroup takes every gridDim.x-th group of rows of its worker and keeps
+// its columns' sums of dy and dy * xh in registers meanwhile: x and dy are read once
+// for all three results.  8 x
 // 2048 rows of 1024 bf16 (101 MB) 20.8 us, and k_norm_params 3.9; 3 x 1111 rows of
 // 4801 f16 (96 MB, and 20 MB of sums) 27.5 and 5.1: a row's two sums over the
 // workgroup come between its loads and its stores, and loads of the next row ahead
 // of them were no faster.
 template <typename T, typename S, int STREAM>
 __global__ __launch_bounds__(S::kThreads, S::kVectors < 3 || S::kThreads > 256 ? 4 : 2) void k_norm_bwd(
-    const T *x, const T *dy, NormArgs a, const float *stats, T *dx, float *part) {
+    const T *x, const T *dy, NormArgs a, const float *stats, T *dx, Sums out) {
     constexpr int kPer = Vec16<T>::kPer, NV = S::kVectors;
     typedef typename Vec16<T>::wide Wide;
     __shared__ float slots[2][2 * 16];
@@ -273,18 +281,27 @@ __global__ __launch_bounds__(S::kThreads, S::kVectors < 3 || S::kThreads > 256 ?
             if (lane < rest && in) *at(out, kPer * vectors + lane) = static_cast<T>(rstd * (last_u - c1 - last_xh * c2));
         }
     }
-    if (!part) return;
     // the workgroup's rows hold the same columns; summed in their order
     constexpr int R = S::kRows, kWidth = S::kLanes * NV * kPer;
     __shared__ float sums[R > 1 ? R : 1][R > 1 ? kWidth : 1], tails[R > 1 ? R : 1][R > 1 ? S::kLanes : 1];
-    float *to = part + (m * gridDim.x + blockIdx.x) * 2 * D;
-    for (int k = 0; k < 2; ++k, to += D) {
+    for (int k = 0; k < 2; ++k) {
+        const int64_t base = k == 0 ? a.gamma : a.beta;
+        if (!out.part && (!out.G || base < 0)) continue;
+        float *to = out.part ? out.part + ((m * gridDim.x + blockIdx.x) * 2 + k) * D : out.G + m * out.ld + base;
+        const bool add = !out.part && out.add;
         if (R == 1) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-                if (lane + S::kLanes * v < vectors)
-                    store_floats<T>(to + kPer * (lane + S::kLanes * v), k == 0 ? sg[v] : sb[v]);
-            if (lane < rest) to[kPer * vectors + lane] = k == 0 ? last_sg : last_sb;
+            for (int v = 0; v < NV; ++v) {
+                if (lane + S::kLanes * v >= vectors) continue;
+                float *at = to + kPer * (lane + S::kLanes * v);
+                Wide s = k == 0 ? sg[v] : sb[v];
+                if (add) s += load_floats<T>(at);
+                store_floats<T>(at, s);
+            }
+            if (lane < rest) {
+                float *at = to + kPer * vectors + lane;
+                *at = (k == 0 ? last_sg : last_sb) + (add ? *at : 0.0f);
+            }
             continue;
         }
         const int r = threadIdx.x / S::kLanes;
@@ -300,7 +317,7 @@ __global__ __launch_bounds__(S::kThreads, S::kVectors < 3 || S::kThreads > 256 ?
             float s = 0.0f;
 #pragma unroll
             for (int q = 0; q < R; ++q) s += tail ? tails[q][c - kPer * vectors] : sums[q][c];
-            to[c] = s;
+            to[c] = add ? to[c] + s : s;
         }
     }
 }
@@ -399,7 +416,14 @@ int64_t forward_groups(int64_t M, int64_t N, int rows_per_group, int threads) {
     const int64_t most = ceil_div(N, rows_per_group), want = ceil_div(threads > 256 ? 2048 : 8192, M);
     return most < want ? most : want;
 }
-int shares_of(int64_t M, int64_t N, int groups, int least) {
+// Shares of a worker's rows whose columns' sums are kept apart.  One where a
+// workgroup comes through all rows in up to 8 turns, and adds its sums to G itself,
+// as the second launch is 3 us of the host's time: 128 rows of 64 bf16 9.2 us and 12.5,
+// 32 of 512 9.0 and 12.3, 8 of 5000 13.3 and 15.8; with 16 turns 64 rows of 1024 would
+// take 18 where shares take 12, 16 of 5000 24 and 16.
+constexpr int64_t kAlone = 8;
+int shares_of(int64_t M, int64_t N, int groups, int least, int rows) {
+    if (ceil_div(N, rows) <= kAlone) return 1;
     const int64_t want = ceil_div(groups, M), most = ceil_div(N, M * N < 8192 ? 8 : least);
     const int64_t s = most < want ? most : want;
     return static_cast<int>(s < 1 ? 1 : s);
@@ -470,13 +494,18 @@ bool with_shape(int64_t D, F &&f) {
     return true;
 }
 
-// Shares of a worker's rows whose columns' sums are kept apart.
-int backward_shares(int64_t M, const dqgan_norm_desc *d) {
-    int shares = shares_of(M, d->tokens, 512, 8);
+// Shares of a call's rows, and whether they are one workgroup's that needs no workspace.
+struct Shares {
+    int count;
+    bool alone;
+};
+Shares backward_shares(int64_t M, const dqgan_norm_desc *d) {
+    Shares shares{shares_of(M, d->tokens, 512, 8, 1), false};
     with_type(d->type, [&](auto t) {
         with_shape<decltype(t), kBackwardMost>(d->width, [&](auto s) {
             using S = decltype(s);
-            shares = shares_of(M, d->tokens, S::kGroups, S::kLeast);
+            shares.count = shares_of(M, d->tokens, S::kGroups, S::kLeast, S::kRows);
+            shares.alone = shares.count == 1;
         });
     });
     return shares;
@@ -525,8 +554,8 @@ dqgan_status dqgan_norm_bytes(dqgan_plan P, const dqgan_norm_desc *d, size_t *by
     DQ_TRY(check(P, d, 0));
     if (!bytes) return DQGAN_EINVAL;
     const bool sums = d->tokens > 0 && (d->gamma >= 0 || d->beta >= 0);
-    *bytes = sums ? sizeof(float) * 2 * static_cast<size_t>(d->width) * P->desc.M * backward_shares(P->desc.M, d)
-                  : 0;
+    const Shares shares = backward_shares(P->desc.M, d);
+    *bytes = sums && !shares.alone ? sizeof(float) * 2 * static_cast<size_t>(d->width) * P->desc.M * shares.count : 0;
     return DQGAN_OK;
 }
 
@@ -541,38 +570,40 @@ dqgan_status dqgan_norm_backward(dqgan_plan P, const dqgan_norm_desc *d, const v
     DQ_TRY(check_ptr(dx, false));
     DQ_TRY(check_ptr(params, any && d->gamma >= 0));
     DQ_TRY(check_ptr(G, sums));
-    DQ_TRY(check_ptr(workspace, any && sums));
+    const Shares shares = any ? backward_shares(P->desc.M, d) : Shares{0, false};
+    DQ_TRY(check_ptr(workspace, any && sums && !shares.alone));
     DQ_TRY(check_device(P));
     hipStream_t st = static_cast<hipStream_t>(stream);
     NormArgs a = args(d, params, ldp);
     const int64_t M = P->desc.M, D = d->width;
-    const int shares = any ? backward_shares(M, d) : 0;
-    float *part = sums ? static_cast<float *>(workspace) : nullptr;
+    const bool alone = sums && shares.alone;
+    float *part = sums && !alone ? static_cast<float *>(workspace) : nullptr;
+    const Sums out{part, alone ? G : nullptr, P->desc.ld, add != 0};
     if (any && (dx || sums)) {
         with_type(d->type, [&](auto t) {
             using T = decltype(t);
             const T *xt = static_cast<const T *>(x), *dyt = static_cast<const T *>(dy);
             T *dxt = static_cast<T *>(dx);
-            const uint32_t my = static_cast<uint32_t>(M), of = static_cast<uint32_t>(shares);
+            const uint32_t my = static_cast<uint32_t>(M), of = static_cast<uint32_t>(shares.count);
             if (with_shape<T, kBackwardMost>(D, [&](auto s) {
                     using S = decltype(s);
                     with_streams(backward_streams(3.0 * sizeof(T) * M * d->tokens * D), [&](auto streams) {
                         k_norm_bwd<T, S, decltype(streams)::value><<<dim3(of, my), S::kThreads, 0, st>>>(
-                            xt, dyt, a, stats, dxt, part);
+                            xt, dyt, a, stats, dxt, out);
                     });
                 }))
                 return;
             if (sums)  // first: dx may be dy
                 k_norm_sums_long<T><<<dim3(static_cast<uint32_t>(ceil_div(D, 2048)), of, my), 256, 0, st>>>(
-                    xt, dyt, a, stats, shares, part);
+                    xt, dyt, a, stats, shares.count, part);
             if (dx)
                 k_norm_bwd_long<T><<<dim3(static_cast<uint32_t>(forward_groups(M, d->tokens, 1, 1024)), my), 1024, 0, st>>>(
                     xt, dyt, a, stats, dxt);
         });
     }
-    if (sums && (any || !add)) {
+    if (sums && !alone && (any || !add)) {
         const dim3 grid(static_cast<uint32_t>(ceil_div(2 * D, 64)), static_cast<uint32_t>(M));
-        k_norm_params<<<grid, 1024, 0, st>>>(part, shares, a, P->desc.ld, G, add != 0);
+        k_norm_params<<<grid, 1024, 0, st>>>(part, shares.count, a, P->desc.ld, G, add != 0);
     }
     return launched();
 }
