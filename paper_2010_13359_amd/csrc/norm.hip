@@ -23,6 +23,10 @@ struct Shape {
         return static_cast<int64_t>(blockIdx.x) * kRows +
                (W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kPerWave : 0);
     }
+    // Whether any lane of this wave has a vector v of a row; the same for the wave.
+    static __device__ __forceinline__ bool any(int v, int vectors) {
+        return (W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64) + kLanes * v < vectors;
+    }
     static __device__ __forceinline__ int row_of_wave() { return kPerWave == 1 ? 0 : (threadIdx.x & 63) / L; }
     // sums over a row's lanes; `slot`: W floats of LDS per value
     static __device__ __forceinline__ float sum(float x, float *slot) {
@@ -67,6 +71,7 @@ struct Row {
         if (vectors > 0) {
 #pragma unroll
             for (int v = 0; v < S::kVectors; ++v) {
+                if (!S::any(v, vectors)) break;
                 const int q = lane + S::kLanes * v;
                 raw[v] = load16<T, STREAM>(at(p, Vec16<T>::kPer * (q < vectors ? q : vectors - 1)));
             }
@@ -117,6 +122,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a
         float last = lane < rest ? widen_bits<T>(row.last) : 0.0f, s = last;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            if (!S::any(v, vectors)) break;
             f[v] = widen<T>(row.raw[v]);
             float part = 0.0f;
 #pragma unroll
@@ -128,6 +134,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a
         s = lane < rest ? last * last : 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            if (!S::any(v, vectors)) break;
             float part = 0.0f;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
@@ -140,6 +147,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a
         T *out = y + (m * a.N + n) * D;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            if (!S::any(v, vectors)) break;
             const int q = lane + S::kLanes * v;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) f[v][i] = fmaf(f[v][i] * rstd, g.of[v][i], b.of[v][i]);
@@ -243,6 +251,7 @@ __global__ __launch_bounds__(S::kThreads, S::kVectors < 3 || S::kThreads > 256 ?
         float s1 = last_u, s2 = last_u * last_xh;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {  // sg and sb of lanes beyond the row are not stored
+            if (!S::any(v, vectors)) break;
             const Wide xv = widen<T>(rx.raw[v]);
             Wide yv = widen<T>(ry.raw[v]);
             if (S::kPerWave > 1 && !in) yv = 0.0f;
@@ -268,6 +277,7 @@ __global__ __launch_bounds__(S::kThreads, S::kVectors < 3 || S::kThreads > 256 ?
             T *out = dx + (m * a.N + n) * D;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
+                if (!S::any(v, vectors)) break;
                 const int q = lane + S::kLanes * v;
                 forget(rx.raw[v]);
                 forget(ry.raw[v]);
