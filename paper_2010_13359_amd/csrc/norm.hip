@@ -7,7 +7,8 @@ namespace {
 
 // Row shapes: L lanes of a wave, or W whole waves, and NV vectors of 16 bytes per
 // lane, so that a row stays in registers between the statistics and their use.
-// The last D % kPer elements lie one each in the row's first lanes.
+// Elements beyond the last whole vector, and beyond NV vectors a lane, lie one each
+// in the row's first lanes.
 template <int L, int W, int NV>
 struct Shape {
     static constexpr int kLanes = W == 1 ? L : 64 * W, kThreads = W < 4 ? 256 : 64 * W, kRows = kThreads / kLanes;
@@ -16,6 +17,15 @@ struct Shape {
     // 2048, 1024 and 512 workgroups rows of 64 bf16 elements (206 MB) take 55, 57 and
     // 81 us, of 2048 (806 MB) 172, 173 and 188, of 4096 (806 MB) 175, 167 and 155.
     static constexpr int kGroups = W == 1 ? 2048 : W * NV <= 4 ? 1024 : 512, kLeast = W == 1 ? 32 : 8;
+    // A row's vectors, and whether the rest fits one element a lane.
+    template <typename T>
+    static __host__ __device__ __forceinline__ int vectors(int64_t D) {
+        return static_cast<int>(D / Vec16<T>::kPer < kLanes * NV ? D / Vec16<T>::kPer : kLanes * NV);
+    }
+    template <typename T>
+    static bool holds(int64_t D) {
+        return D <= static_cast<int64_t>(kLanes) * (NV * Vec16<T>::kPer + 1);
+    }
     static constexpr int kVectors = NV, kPerWave = W == 1 ? 64 / L : 1;  // rows a wave holds
     // The first row of this wave's, in a scalar register: a loop over it keeps one
     // set of sums.
@@ -107,7 +117,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a
     __shared__ float slots[2][16];
     const int lane = threadIdx.x % S::kLanes;
     const int64_t m = blockIdx.y, D = a.D;
-    const int vectors = static_cast<int>(D / kPer), rest = static_cast<int>(D % kPer);
+    const int vectors = S::template vectors<T>(D), rest = static_cast<int>(D) - kPer * vectors;
     Params<T, S> g, b;
     g.load(a.P + m * a.ldp + a.gamma, 1.0f, a.gamma >= 0, lane, vectors, rest);
     b.load(a.P + m * a.ldp + a.beta, 0.0f, a.beta >= 0, lane, vectors, rest);
@@ -222,7 +232,7 @@ __global__ __launch_bounds__(S::kThreads, S::kVectors < 3 || S::kThreads > 256 ?
     __shared__ float slots[2][2 * 16];
     const int lane = threadIdx.x % S::kLanes;
     const int64_t m = blockIdx.y, D = a.D;
-    const int vectors = static_cast<int>(D / kPer), rest = static_cast<int>(D % kPer);
+    const int vectors = S::template vectors<T>(D), rest = static_cast<int>(D) - kPer * vectors;
     Params<T, S> g;
     g.load(a.P + m * a.ldp + a.gamma, 1.0f, a.gamma >= 0, lane, vectors, rest);
     Wide sg[NV], sb[NV];
@@ -475,33 +485,21 @@ NormArgs args(const dqgan_norm_desc *d, const float *P, int64_t ldp) {
 // f(Shape{}) with the smallest row shape that holds D elements of T; returns
 // false, f not called, if D is above MOST.  16 waves of four vectors have 128
 // registers a lane, too few for the backward pass of 16-bit types.
+template <typename S, typename T, typename F>
+bool if_holds(int64_t D, F &f) {
+    if (!S::template holds<T>(D)) return false;
+    f(S{});
+    return true;
+}
 template <typename T, int MOST, typename F>
 bool with_shape(int64_t D, F &&f) {
-    const int64_t vectors = D / Vec16<T>::kPer;
-    if (vectors <= 16)
-        f(Shape<16, 1, 1>{});
-    else if (vectors <= 32)
-        f(Shape<16, 1, 2>{});
-    else if (vectors <= 64)
-        f(Shape<64, 1, 1>{});
-    else if (vectors <= 128)
-        f(Shape<64, 1, 2>{});
-    else if (vectors <= 256)
-        f(Shape<64, 4, 1>{});
-    else if (vectors <= 512)
-        f(Shape<64, 4, 2>{});
-    else if (vectors <= 768)
-        f(Shape<64, 4, 3>{});
-    else if (vectors <= 1024)
-        f(Shape<64, 4, 4>{});
-    else if (vectors <= 2048)
-        f(Shape<64, 16, 2>{});
-    else if constexpr (MOST / Vec16<T>::kPer > 2048) {
-        if (vectors > 4096 || D > MOST) return false;
-        f(Shape<64, 16, 4>{});
-    } else
-        return false;
-    return true;
+    if (D > MOST) return false;
+    if (if_holds<Shape<16, 1, 1>, T>(D, f) || if_holds<Shape<16, 1, 2>, T>(D, f) || if_holds<Shape<64, 1, 1>, T>(D, f) ||
+        if_holds<Shape<64, 1, 2>, T>(D, f) || if_holds<Shape<64, 4, 1>, T>(D, f) || if_holds<Shape<64, 4, 2>, T>(D, f) ||
+        if_holds<Shape<64, 4, 3>, T>(D, f) || if_holds<Shape<64, 4, 4>, T>(D, f) || if_holds<Shape<64, 16, 2>, T>(D, f))
+        return true;
+    if constexpr (MOST / Vec16<T>::kPer > 2048) return if_holds<Shape<64, 16, 4>, T>(D, f);
+    return false;
 }
 
 // Shares of a call's rows, and whether they are one workgroup's that needs no workspace.

@@ -8,7 +8,8 @@ import layer_refs as ref
 pytestmark = pytest.mark.gpu
 
 WIDTHS = [1, 2, 7, 8, 9, 63, 64, 65, 300, 511, 512, 513, 1000, 1023, 1024, 1025, 2047, 2048, 2049, 4095, 4096, 4097, 8192,
-          8193, 16384, 16385, 32768, 32769, 40001]
+          8193, 16384, 16385, 32768, 32769, 40001] + [80, 81, 144, 145, 272, 273, 576, 577, 1088, 1089, 1280, 1281, 2304,
+                                                      2305, 4352, 4353, 8448, 8449, 17408, 17409]
 
 
 def _setup(M, N, D, dt, gamma, beta, seed=0, kind="normal"):
