@@ -495,7 +495,7 @@ template <typename T, int MOST, typename F>
 bool with_shape(int64_t D, F &&f) {
     if (D > MOST) return false;
     if (if_holds<Shape<16, 1, 1>, T>(D, f) || if_holds<Shape<16, 1, 2>, T>(D, f) || if_holds<Shape<64, 1, 1>, T>(D, f) ||
-        if_holds<Shape<64, 1, 2>, T>(D, f) || if_holds<Shape<64, 4, 1>, T>(D, f) || if_holds<Shape<64, 4, 2>, T>(D, f) ||
+        if_holds<Shape<64, 1, 2>, T>(D, f) || if_holds<Shape<64, 1, 3>, T>(D, f) || if_holds<Shape<64, 4, 1>, T>(D, f) || if_holds<Shape<64, 4, 2>, T>(D, f) ||
         if_holds<Shape<64, 4, 3>, T>(D, f) || if_holds<Shape<64, 4, 4>, T>(D, f) || if_holds<Shape<64, 16, 2>, T>(D, f))
         return true;
     if constexpr (MOST / Vec16<T>::kPer > 2048) return if_holds<Shape<64, 16, 4>, T>(D, f);
