@@ -47,11 +47,11 @@ template <typename T>
 constexpr int forward_rows = sizeof(T) == 4 ? 2 : 4;
 template <typename T, typename I, bool STREAM>
 __global__ __launch_bounds__(256) void k_embed_fwd(const I *tok, const float *P, int64_t ldp, EmbedArgs a, int shift,
-                                                   T *out) {
+                                                   int64_t vectors, T *out) {
     constexpr int kRows = forward_rows<T>;
     typedef T Four __attribute__((ext_vector_type(4)));
     typedef T FourAnywhere __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    const int64_t m = blockIdx.y, vectors = a.D >> 2;
+    const int64_t m = blockIdx.y;
     const int lanes = 1 << shift, per = 256 >> shift, lane = threadIdx.x & (lanes - 1);
     const float *table = P + m * ldp + a.offset;
     tok += m * a.N;
@@ -84,7 +84,8 @@ __global__ __launch_bounds__(256) void k_embed_fwd(const I *tok, const float *P,
             }
         }
         const int64_t c = 4 * vectors + lane;
-        if (lane < 4 && c < a.D) {
+        if (c < a.D) {
+#pragma unroll
             for (int u = 0; u < kRows; ++u)
                 if (n + u * per < a.N)
                     out[(n + u * per) * a.D + c] = static_cast<T>(there[u] ? row[u][c] * a.scale : 0.0f);
@@ -734,8 +735,14 @@ dqgan_status dqgan_embed_forward(dqgan_plan P, const dqgan_embed_desc *d, const 
     if (!any) return DQGAN_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const EmbedArgs a = args(P, d);
-    int shift = 2;  // at least the four lanes of the last D % 4 channels
-    while (shift < 8 && (int64_t(4) << shift) < a.D) ++shift;
+    // At least the four lanes of the last D % 4 channels; from 32 lanes on, one more
+    // channel for up to half of them: 11 x 50469 tokens, rows of 561 to bf16 233 us, 275
+    // with 256 lanes for 140 vectors; rows of 138 105 and 119.  With one more for all of
+    // them rows of 1280 lose (83 us and 73), with 16 lanes those of 71 (162 and 146).
+    const auto reach = [](int64_t lanes) { return 4 * lanes + (lanes >= 32 ? lanes / 2 : 0); };
+    int shift = 2;
+    while (shift < 8 && reach(int64_t(1) << shift) < a.D) ++shift;
+    const int64_t lanes = int64_t(1) << shift, vectors = a.D <= reach(lanes) && a.D > 4 * lanes ? lanes : a.D >> 2;
     with_type(d->type, [&](auto t) {
         with_index(d->index_type, [&](auto i) {
             using T = decltype(t);
@@ -743,10 +750,10 @@ dqgan_status dqgan_embed_forward(dqgan_plan P, const dqgan_embed_desc *d, const 
             const int64_t groups = ceil_div(a.N, forward_rows<T> * (256 >> shift));
             const dim3 grid(static_cast<uint32_t>(groups < 65536 ? groups : 65536), static_cast<uint32_t>(P->desc.M));
             if (forward_streams(static_cast<double>(sizeof(T)) * P->desc.M * a.N * a.D))
-                k_embed_fwd<T, I, true><<<grid, 256, 0, st>>>(static_cast<const I *>(tok), params, ldp, a, shift,
+                k_embed_fwd<T, I, true><<<grid, 256, 0, st>>>(static_cast<const I *>(tok), params, ldp, a, shift, vectors,
                                                               static_cast<T *>(out));
             else
-                k_embed_fwd<T, I, false><<<grid, 256, 0, st>>>(static_cast<const I *>(tok), params, ldp, a, shift,
+                k_embed_fwd<T, I, false><<<grid, 256, 0, st>>>(static_cast<const I *>(tok), params, ldp, a, shift, vectors,
                                                                static_cast<T *>(out));
         });
     });
