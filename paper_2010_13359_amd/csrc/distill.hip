@@ -283,7 +283,8 @@ constexpr int kTwoVectors = 12, kTwoHeld = 4;
 // the others on its CU; one workgroup a CU that asks for the next row meanwhile was
 // slower than two that do not.
 template <typename T, int W, int NV, int NL, bool LOSS, bool GRAD, bool STREAM>
-__global__ __launch_bounds__(64 * W, NV == kTwoVectors ? 8 : 1) void k_distill_row(const T *z, DistillArgs a, float *loss, float *stats, T *dz) {
+__global__ __launch_bounds__(64 * W, NV == kTwoVectors ? 8 : 1) void k_distill_row(const T *z, DistillArgs a, float *loss,
+                                                                                   float *stats, T *dz) {
     constexpr bool FINE = sizeof(T) == 4;
     constexpr int kPer = Vec16<T>::kPer;
     __shared__ Message s;

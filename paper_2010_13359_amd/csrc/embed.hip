@@ -702,9 +702,11 @@ void with_index(int32_t type, F &&f) {
         f(int64_t{});
 }
 
-// Whether `out` passes by the caches: 134 MB 47.3 us so and 52.8 not, 33 MB 13.4
-// and 15.7 (rows of 501 bf16: 15.1 and 14.1), 17 MB the same.
-bool forward_streams(double bytes) { return bytes > 30e6; }
+// Whether `out` passes by the caches: 134 MB 47 us so and 53 not, 33 MB 13.4 and
+// 15.7 (rows of 501 bf16: 15.1 and 14.1), 17 MB the same.  Not narrow rows with
+// single channels behind the last four, whose lines come in many pieces: 1.6 million
+// of 35 f32 127 us and 90, 1.2 million of 71 bf16 145 and 128, of 117 156 and 153.
+bool forward_streams(double bytes, int64_t D) { return bytes > 30e6 && (D % 4 == 0 || D >= 100); }
 // Whether dout passes by the caches: 268 MB 148 us (the whole gradient) so and 181
 // not, 134 MB 356 and 365, 33 MB 118 and 114.
 bool backward_streams(double bytes) { return bytes > 100e6; }
@@ -749,7 +751,7 @@ dqgan_status dqgan_embed_forward(dqgan_plan P, const dqgan_embed_desc *d, const 
             using I = decltype(i);
             const int64_t groups = ceil_div(a.N, forward_rows<T> * (256 >> shift));
             const dim3 grid(static_cast<uint32_t>(groups < 65536 ? groups : 65536), static_cast<uint32_t>(P->desc.M));
-            if (forward_streams(static_cast<double>(sizeof(T)) * P->desc.M * a.N * a.D))
+            if (forward_streams(static_cast<double>(sizeof(T)) * P->desc.M * a.N * a.D, a.D))
                 k_embed_fwd<T, I, true><<<grid, 256, 0, st>>>(static_cast<const I *>(tok), params, ldp, a, shift, vectors,
                                                               static_cast<T *>(out));
             else
