@@ -330,3 +330,81 @@ def test_many_elements():
     w = ref.norm_forward(rows, P[0, :D], P[0, D:2 * D], 1e-5)
     ref.check("y", x[0, -2:], w[0], w[1])
     plan.close()
+
+
+# ---------------------------------------------------------------------------
+# most workers, widest rows
+
+
+@pytest.mark.parametrize("N", [2, 230])
+def test_most_workers(N):
+    import torch
+    from paper_2010_13359_amd import layers
+    M, V, D, k = 1024, 21, 13, 5
+    where = dict(gamma=V * D, beta=V * D + D)
+    plan = ref.plan(V * D + 2 * D, M)
+    gen = torch.Generator().manual_seed(N)
+    P = torch.randn((M, plan.ld), generator=gen).cuda()
+    tok = torch.randint(-1, V + 1, (M, N), generator=gen).int().cuda()
+    dy = torch.randn((M, N, D), generator=gen).cuda()
+    z, val = torch.randn((M, N, V), generator=gen).cuda(), torch.randn((M, N, k), generator=gen).cuda()
+    idx = torch.randint(0, V + 2, (M, N, k), generator=gen).int().cuda()
+    x, y, dx, dz = torch.empty_like(dy), torch.empty_like(dy), torch.empty_like(dy), torch.empty_like(z)
+    stats, loss = torch.empty((M, N, 2), device="cuda"), torch.empty((M, N), device="cuda")
+    G = torch.full((M, plan.ld), 7.0, device="cuda")
+    layers.embed_forward(plan, tok, P, x, V)
+    layers.norm_forward(plan, x, P, y, stats, **where)
+    layers.norm_backward(plan, x, dy, P, stats, dx, G, layers.norm_workspace(plan, N, D, x.dtype, **where), **where)
+    layers.embed_backward(plan, tok, dx, G, V, layers.embed_workspace(plan, N, V, D, x.dtype))
+    layers.distill_fused(plan, z, val, idx, None, loss, dz)
+    for m in (0, 1, 500, 1022, 1023):
+        gamma, beta = P[m, V * D:V * D + D], P[m, V * D + D:V * D + 2 * D]
+        w = ref.embed_forward(tok[m], P[m, :V * D].view(V, D), 1.0)
+        ref.check("x", x[m], w[0], w[1])
+        w = ref.norm_forward(x[m], gamma, beta, 1e-5)
+        ref.check("y", y[m], w[0], w[1])
+        w = ref.norm_backward(x[m], dy[m], gamma, stats[m])
+        ref.check("dx", dx[m], w[0], w[1])
+        ref.check("dgamma", G[m, V * D:V * D + D], w[2], w[3])
+        ref.check("dbeta", G[m, V * D + D:V * D + 2 * D], w[4], w[5])
+        w = ref.embed_backward(tok[m], dx[m], V, 1.0)
+        ref.check("dE", G[m, :V * D].view(V, D), w[0], w[1])
+        w = ref.distill(z[m], val[m], idx[m], None, V, 1.0)
+        ref.check("loss", loss[m], w["loss"], w["loss_err"])
+        ref.check("dz", dz[m], w["dz"], w["dz_err"])
+    assert bool((G[:, V * D + 2 * D:] == 7.0).all())
+    plan.close()
+
+
+def test_widest_rows():
+    """Rows of 2^24 elements; a width beyond is refused."""
+    import torch
+    from paper_2010_13359_amd import dqgan, layers
+    D = 1 << 24
+    gen = torch.Generator().manual_seed(6)
+    plan = ref.plan(2 * D + 1, 1)
+    P = torch.randn((1, plan.ld), generator=gen).cuda()
+    G = torch.full((1, plan.ld), 7.0, device="cuda")
+    tok = torch.tensor([[1, 0, 1]], device="cuda")
+    x, dy = torch.empty((1, 3, D), dtype=torch.bfloat16, device="cuda"), torch.randn((1, 3, D), generator=gen).bfloat16().cuda()
+    print("embedding", flush=True)
+    layers.embed_forward(plan, tok, P, x, 2)
+    w = ref.embed_forward(tok[0], P[0, :2 * D].view(2, D), 1.0)
+    ref.check("x", x[0], w[0], w[1])
+    layers.embed_backward(plan, tok, dy, G, 2, layers.embed_workspace(plan, 3, 2, D, x.dtype))
+    w = ref.embed_backward(tok[0], dy[0], 2, 1.0)
+    ref.check("dE", G[0, :2 * D].view(2, D), w[0], w[1])
+    assert bool((G[:, 2 * D:] == 7.0).all())
+    print("layer norm", flush=True)
+    y, dx, stats = torch.empty_like(x), torch.empty_like(x), torch.empty((1, 3, 2), device="cuda")
+    layers.norm_forward(plan, x, P, y, stats, gamma=1, beta=D + 1)
+    w = ref.norm_forward(x[0], P[0, 1:D + 1], P[0, D + 1:2 * D + 1], 1e-5)
+    ref.check("y", y[0], w[0], w[1])
+    layers.norm_backward(plan, x, dy, P, stats, dx, G, layers.norm_workspace(plan, 3, D, x.dtype, 1, D + 1), 1, D + 1)
+    w = ref.norm_backward(x[0], dy[0], P[0, 1:D + 1], stats[0])
+    ref.check("dx", dx[0], w[0], w[1])
+    ref.check("dgamma", G[0, 1:D + 1], w[2], w[3])
+    with pytest.raises(dqgan.DqganError) as e:
+        layers.embed_forward(plan, tok[:, :1], P, torch.empty((1, 1, D + 1), device="cuda"), 1)
+    assert e.value.status == dqgan.EINVAL
+    plan.close()
