@@ -442,9 +442,13 @@ int64_t forward_groups(int64_t M, int64_t N, int rows_per_group, int threads) {
 // 32 of 512 9.0 and 12.3, 8 of 5000 13.3 and 15.8; with 16 turns 64 rows of 1024 would
 // take 18 where shares take 12, 16 of 5000 24 and 16.
 constexpr int64_t kAlone = 8;
-int shares_of(int64_t M, int64_t N, int groups, int least, int rows) {
+// Otherwise 8 rows at least, and 4 of those that take a workgroup each while there
+// are CUs for all (1000 rows of 4096 f16 14.7 us and 18.2, 500 of 12288 19.7 and 26.2;
+// 2 x 1000 of 12288 52 and 43).
+int shares_of(int64_t M, int64_t N, int groups, int least, int rows, int threads) {
     if (ceil_div(N, rows) <= kAlone) return 1;
-    const int64_t want = ceil_div(groups, M), most = ceil_div(N, M * N < 8192 ? 8 : least);
+    const bool short_ones = rows == 1 && M * ceil_div(N, 4) <= (threads > 256 ? 256 : 512);
+    const int64_t want = ceil_div(groups, M), most = ceil_div(N, short_ones ? 4 : M * N < 8192 ? 8 : least);
     const int64_t s = most < want ? most : want;
     return static_cast<int>(s < 1 ? 1 : s);
 }
@@ -508,11 +512,11 @@ struct Shares {
     bool alone;
 };
 Shares backward_shares(int64_t M, const dqgan_norm_desc *d) {
-    Shares shares{shares_of(M, d->tokens, 512, 8, 1), false};
+    Shares shares{shares_of(M, d->tokens, 512, 8, 1, 1024), false};
     with_type(d->type, [&](auto t) {
         with_shape<decltype(t), kBackwardMost>(d->width, [&](auto s) {
             using S = decltype(s);
-            shares.count = shares_of(M, d->tokens, S::kGroups, S::kLeast, S::kRows);
+            shares.count = shares_of(M, d->tokens, S::kGroups, S::kLeast, S::kRows, S::kThreads);
             shares.alone = shares.count == 1;
         });
     });
