@@ -78,6 +78,13 @@ def test_student_runs_with_every_compressor(kind, extra):
     assert len(hist) == 6 and np.isfinite(hist).all() and min(hist) > 0
 
 
+def test_student_in_16_bits():
+    import torch
+    from paper_2010_13359_amd import closed_loop
+    hist = closed_loop.run_student("sign", vocab=1000, width=96, tokens=300, T=4, temperature=2.0, dtype=torch.bfloat16)
+    assert len(hist) == 4 and np.isfinite(hist).all() and min(hist) > 0
+
+
 # ---------------------------------------------------------------------------
 # graphs and streams
 
