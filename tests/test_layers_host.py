@@ -59,7 +59,7 @@ def _embed(**kw):
 
 def _norm(**kw):
     from paper_2010_13359_amd import layers
-    base = dict(gamma=10, beta=100, width=64, tokens=7, eps=1e-5, type=1, reserved=0)
+    base = dict(gamma=10, beta=100, width=64, tokens=1000, eps=1e-5, type=1, reserved=0)
     base.update(kw)
     return layers.NormDesc(*base.values())
 
