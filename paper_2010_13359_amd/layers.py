@@ -76,7 +76,8 @@ def _type(dtype, name):
 
 
 # descriptors by their values and the plan's sizes, with the workspace that the
-# library asks for: neither depends on anything else
+# library asks for: neither depends on anything else (-0.0 as a scale is 0.0, its
+# equal as a key)
 _descs = {}
 
 
@@ -158,7 +159,7 @@ def _embed(plan, tokens, x, name, vocab, offset, scale):
     """Descriptor, workspace, pointers of the tokens and of the activations x."""
     at, shape, dtype = _sizes(plan, x, name)
     tok = _like(plan, tokens, "tokens", shape[:2], INDEX_TYPES)
-    d, need = _desc(plan, EmbedDesc, "dqgan_embed_bytes", offset, vocab, shape[2], shape[1], scale, TYPES[dtype],
+    d, need = _desc(plan, EmbedDesc, "dqgan_embed_bytes", offset, vocab, shape[2], shape[1], scale + 0.0, TYPES[dtype],
                     0 if tokens is None else INDEX_TYPES[tokens.dtype], 0)
     return d, need, tok, at
 
