@@ -92,7 +92,8 @@ typedef struct {
  * of each row (var: the mean square of x - mean, which has to be within binary32;
  * a row of equal elements needs eps > 0).
  *   x, y [M][tokens][width]; y may be x.
- *   stats [M][tokens][2] fp32 (mean, rstd) or NULL.
+ *   stats [M][tokens][2] fp32 (mean, rstd) or NULL.  y is not made from the rounded
+ *   mean: rows far from zero for their deviation keep their digits.
  *   P may be NULL if there is neither weight nor bias. */
 dqgan_status dqgan_norm_forward(dqgan_plan plan, const dqgan_norm_desc *desc, const void *x, const float *P,
                                 int64_t ldp, void *y, float *stats, void *stream);
@@ -105,7 +106,9 @@ dqgan_status dqgan_norm_bytes(dqgan_plan plan, const dqgan_norm_desc *desc, size
  *   dx = rstd * (u - mean(u) - xh * mean(u * xh))      (means over the row)
  *   G[m][gamma + c] (+)= sum over n of dy * xh,  G[m][beta + c] (+)= sum over n of dy.
  *   dx may be NULL (not wanted) or dy.  G may be NULL if there is neither
- *   weight nor bias, P if there is no weight.  stats: what the forward pass left. */
+ *   weight nor bias, P if there is no weight.  stats: what the forward pass left;
+ *   xh is that of the given mean and rstd (a mean rounded to binary32 shifts the xh
+ *   of its row by up to 2^-24 |mean| rstd). */
 dqgan_status dqgan_norm_backward(dqgan_plan plan, const dqgan_norm_desc *desc, const void *x, const void *dy,
                                  const float *P, int64_t ldp, const float *stats, void *dx, float *G, int32_t add,
                                  void *workspace, void *stream);

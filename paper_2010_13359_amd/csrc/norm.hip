@@ -106,15 +106,39 @@ struct Params {
     }
 };
 
+// What y is made of.  The mean in binary32 is off by some units of its last place,
+// which matters to rows that lie far from zero for their deviation: of 1000 elements
+// about 10^4 with a deviation of 0.01 the variance would be off by 0.3 % and y by
+// 0.05.  Such rows (the mean above eight deviations) take the mean r of x - mean too,
+// and y and the variance about mean + r: off by 1e-7 and 3e-7.  Of the others y is off
+// by at most 8 (depth of the sum) 2^-24 for it, and they cost one comparison (8 x 4000
+// rows of 9000 bf16, one in a hundred of them far, 262 us; without r 254, with r for
+// all rows 279; 32 x 16384 of 64 29, 28 and 31).
+constexpr float kFar = 64.0f;  // the square of eight
+struct Centre {
+    float var, rstd, r = 0.0f, shift = 0.0f;
+    bool far;
+    __device__ __forceinline__ Centre(float mean, float squares, float eps)
+        : var(squares), rstd(1.0f / sqrtf(squares + eps)), far(mean * mean > kFar * (squares + eps)) {}
+    __device__ __forceinline__ void correct(float rest, float eps) {
+        r = rest;
+        const float v = fmaf(-r, r, var);
+        rstd = 1.0f / sqrtf((v < 0.0f ? 0.0f : v) + eps);  // just below 0: equal elements
+        shift = -r * rstd;
+    }
+    // of an element from which the computed mean has been taken
+    __device__ __forceinline__ float normal(float f) const { return fmaf(f, rstd, shift); }
+};
+
 // Two passes over the registers: the mean, then the mean square of what is
-// left, so that a large mean costs the variance no digits.  Bound by memory: 8 x
+// left.  Bound by memory: 8 x
 // 8192 rows of 2048 bf16 (537 MB) 95 us, 5.7 TB/s of the 6.1 of a large copy; few
 // rows are one launch and two sums over a wave, 2.7 us.
 template <typename T, typename S, int STREAM>
 __global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a, T *y, float *stats) {
     constexpr int kPer = Vec16<T>::kPer, NV = S::kVectors;
     typedef typename Vec16<T>::wide Wide;
-    __shared__ float slots[2][16];
+    __shared__ float slots[3][16];
     const int lane = threadIdx.x % S::kLanes;
     const int64_t m = blockIdx.y, D = a.D;
     const int vectors = S::template vectors<T>(D), rest = static_cast<int>(D) - kPer * vectors;
@@ -153,28 +177,41 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a
             }
             s += lane + S::kLanes * v < vectors ? part : 0.0f;
         }
-        const float rstd = 1.0f / sqrtf(S::sum(s, slots[1]) * inv + a.eps);
+        Centre centre(mean, S::sum(s, slots[1]) * inv, a.eps);
+        if (__any(centre.far)) {  // of one row for all waves, or of this wave's rows
+            s = lane < rest ? last : 0.0f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                if (!S::any(v, vectors)) break;
+                float part = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) part += f[v][i];
+                s += lane + S::kLanes * v < vectors ? part : 0.0f;
+            }
+            const float r = S::sum(s, slots[2]) * inv;
+            if (centre.far) centre.correct(r, a.eps);
+        }
         T *out = y + (m * a.N + n) * D;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             if (!S::any(v, vectors)) break;
             const int q = lane + S::kLanes * v;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) f[v][i] = fmaf(f[v][i] * rstd, g.of[v][i], b.of[v][i]);
+            for (int i = 0; i < kPer; ++i) f[v][i] = fmaf(centre.normal(f[v][i]), g.of[v][i], b.of[v][i]);
             if (q < vectors && in) store16<T, (STREAM > 0)>(at(out, kPer * q), narrow<T>(f[v]));
         }
-        if (lane < rest && in) *at(out, kPer * vectors + lane) = static_cast<T>(fmaf(last * rstd, g.last, b.last));
+        if (lane < rest && in) *at(out, kPer * vectors + lane) = static_cast<T>(fmaf(centre.normal(last), g.last, b.last));
         if (stats && lane == 0 && in) {
-            stats[2 * (m * a.N + n)] = mean;
-            stats[2 * (m * a.N + n) + 1] = rstd;
+            stats[2 * (m * a.N + n)] = mean + centre.r;
+            stats[2 * (m * a.N + n) + 1] = centre.rstd;
         }
     }
 }
 
-// Rows that do not fit the registers: read three times.
+// Rows that do not fit the registers: read three times, four if far from zero.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_norm_fwd_long(const T *x, NormArgs a, T *y, float *stats) {
-    __shared__ float slots[2][16];
+    __shared__ float slots[3][16];
     const int64_t m = blockIdx.y, D = a.D;
     const float inv = 1.0f / static_cast<float>(D);
     for (int64_t n = blockIdx.x; n < a.N; n += gridDim.x) {
@@ -192,19 +229,28 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const T *x, NormArgs a, 
 #pragma unroll
             for (int i = 0; i < 8; ++i) s = fmaf(f[i] - mean, f[i] - mean, s);
         }
-        const float rstd = 1.0f / sqrtf(group_sum<16>(s, slots[1]) * inv + a.eps);
+        Centre centre(mean, group_sum<16>(s, slots[1]) * inv, a.eps);
+        if (centre.far) {  // the same for all waves
+            s = 0.0f;
+            for (int64_t c = 8 * threadIdx.x; c < D; c += 8192) {
+                const f32x8 f = load8(row + c, D - c, mean);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += f[i] - mean;
+            }
+            centre.correct(group_sum<16>(s, slots[2]) * inv, a.eps);
+        }
         T *out = y + (m * a.N + n) * D;
         for (int64_t c = 8 * threadIdx.x; c < D; c += 8192) {
             f32x8 f = load8(row + c, D - c), g = 1.0f, b = 0.0f;
             if (a.gamma >= 0) g = load8(a.P + m * a.ldp + a.gamma + c, D - c);
             if (a.beta >= 0) b = load8(a.P + m * a.ldp + a.beta + c, D - c);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = fmaf((f[i] - mean) * rstd, g[i], b[i]);
+            for (int i = 0; i < 8; ++i) f[i] = fmaf(centre.normal(f[i] - mean), g[i], b[i]);
             store8(out + c, D - c, f);
         }
         if (stats && threadIdx.x == 0) {
-            stats[2 * (m * a.N + n)] = mean;
-            stats[2 * (m * a.N + n) + 1] = rstd;
+            stats[2 * (m * a.N + n)] = mean + centre.r;
+            stats[2 * (m * a.N + n) + 1] = centre.rstd;
         }
     }
 }

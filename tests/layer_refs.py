@@ -96,6 +96,34 @@ def norm_forward(x, gamma, beta, eps):
     return y, y_err, mean[:, 0], mean_err[:, 0], rstd[:, 0], (rstd * rstd_rel)[:, 0]
 
 
+def norm_forward_centred(x, gamma, beta, eps):
+    """As norm_forward, with the bounds of a row whose mean m in binary32 (off by at
+    most `off`) is corrected by the mean r of the f = x - m: f has one rounding, r
+    those of its sum and two more, the variance mean(f^2) - r^2 those of both and one
+    more, and y is taken from f and r in 32 bits."""
+    x = x.double().cpu()
+    D = x.shape[1]
+    k = depth(D)
+    g = torch.ones(D, dtype=torch.float64) if gamma is None else gamma.double().cpu()
+    b = torch.zeros(D, dtype=torch.float64) if beta is None else beta.double().cpu()
+    e = float(torch.tensor(eps, dtype=torch.float32))
+    mean = x.mean(1, keepdim=True)
+    xc = x - mean
+    var = (xc * xc).mean(1, keepdim=True)
+    rstd = 1.0 / torch.sqrt(var + e)
+    off = (k + 2) * U * x.abs().mean(1, keepdim=True)
+    size = xc.abs() + off                               # of f
+    r_err = (k + 4) * U * size.mean(1, keepdim=True)
+    var_err = (k + 7) * U * (size * size).mean(1, keepdim=True) + 2 * off * r_err + r_err ** 2 + U * off ** 2
+    rstd_rel = var_err / (2 * (var + e - var_err).clamp(min=1e-300)) + 4 * U
+    xh = xc * rstd
+    # f's rounding, r's error, the roundings of r * rstd and of the result; rstd's own
+    xh_err = (rstd * (U * size + r_err + U * (off + r_err)) + 2 * U * xh.abs()) * (1 + rstd_rel) + xh.abs() * rstd_rel
+    y = xh * g + b
+    y_err = g.abs() * xh_err + U * (y.abs() + g.abs() * xh_err)
+    return y, y_err, mean[:, 0], (r_err + U * (mean.abs() + r_err))[:, 0], rstd[:, 0], (rstd * rstd_rel)[:, 0]
+
+
 def norm_backward(x, dy, gamma, stats):
     """[N][D], stats [N][2] as given: (dx, error, dgamma, error, dbeta, error)."""
     x, dy = x.double().cpu(), dy.double().cpu()

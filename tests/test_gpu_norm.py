@@ -179,3 +179,31 @@ def test_gradients_against_differences(D):
     size = float((dx.double().cpu() * ex).abs().sum() + (G[0, :2 * D].double().cpu().view(2, D) * ep).abs().sum())
     assert abs(slope - mine) <= size * (h * h * 8 + (ref.depth(D) + 12) * ref.U)
     pl.close()
+
+
+@pytest.mark.parametrize("kind", ["far", "equal", "one apart"])
+@pytest.mark.parametrize("dt", sorted(ref.TYPES))
+@pytest.mark.parametrize("D", [5, 60, 200, 1000, 1023, 1500, 2049, 3001, 6000, 9000, 20000, 40001])
+def test_a_large_mean_costs_no_digits(D, dt, kind):
+    """Rows far from zero against the deviation they have, of one value, and of one
+    value but for one element: the mean's own rounding is in neither y nor rstd."""
+    import torch
+    from paper_2010_13359_amd import layers
+    gen = torch.Generator().manual_seed(D)
+    base = torch.tensor([1e4, -37.3, 1e3, 100.0 / 3, 0.7, 1e4 + 1.0 / 3]).view(1, 6, 1)
+    pl, _, P, _ = _setup(1, 1, D, dt, 0, D, seed=D)
+    x = base.expand(1, 6, D).clone()
+    if kind == "far":
+        x += 1e-6 * base.abs() * torch.randn(x.shape, generator=gen)
+    x = x.to(ref.TYPES[dt])
+    if kind == "one apart":
+        x[..., D // 2] *= 1.01
+    x = x.cuda()
+    eps = 1e-12 if dt == "f32" and kind != "equal" else 1e-5       # rows of one value have no other variance
+    y, stats = torch.full_like(x, float("nan")), torch.full((1, 6, 2), float("nan"), device="cuda")
+    layers.norm_forward(pl, x, P, y, stats, gamma=1, beta=D + 3, eps=eps)
+    w = ref.norm_forward_centred(x[0], P[0, 1:D + 1], P[0, D + 3:2 * D + 3], eps)
+    ref.check("y", y[0], w[0], w[1])
+    ref.check("mean", stats[0, :, 0], w[2], w[3])
+    ref.check("rstd", stats[0, :, 1], w[4], w[5])
+    pl.close()
