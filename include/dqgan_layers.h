@@ -55,7 +55,8 @@ typedef struct {
                            [vocab][width], offset + vocab * width <= d               */
     int64_t vocab;      /* 1 <= vocab <= 2^31 - 2                                    */
     int64_t width;      /* 1 <= width <= 2^24                                        */
-    int64_t tokens;     /* per worker, 0 <= tokens <= 2^30                           */
+    int64_t tokens;     /* per worker, 0 <= tokens <= 2^30; activations of one worker
+                           that come to a terabyte (2^40 bytes) may be refused        */
     float scale;        /* finite                                                    */
     int32_t type;       /* dqgan_type of out and dout                                */
     int32_t index_type; /* dqgan_index_type of tok                                   */

@@ -629,7 +629,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(const uint32_t *
 
 // ---------------------------------------------------------------------------
 
-constexpr int64_t kMostGroups = int64_t(1) << 24;  // of 256 threads in a launch's first dimension: below 2^32 threads
+constexpr int64_t kMostGroups = int64_t(1) << 24;  // bound of a launch's workgroups of 256 threads: 2^32 threads
 
 // The vectors of a row in equal shares of up to 64, one per wave.
 int slabs_of(int64_t D, int per) {
@@ -686,7 +686,9 @@ dqgan_status check(dqgan_plan P, const dqgan_embed_desc *d) {
     if (d->offset < 0 || d->offset >= n || d->vocab > (n - d->offset) / d->width) return DQGAN_EINVAL;
     if (!tokens_ok(P, d->tokens) || !type_ok(d->type) || d->reserved != 0 || !isfinite(d->scale)) return DQGAN_EINVAL;
     if (d->index_type != DQGAN_I32 && d->index_type != DQGAN_I64) return DQGAN_EINVAL;
-    if (ceil_div(d->tokens, kChunkLong) * slabs_of(d->width, 4) > kMostGroups) return DQGAN_EINVAL;
+    // k_embed_join's workgroups of 512 threads, and with them k_embed_sum's of 256
+    const int64_t slabs = slabs_of(d->width, d->type == DQGAN_F32 ? 4 : 8);
+    if (ceil_div(ceil_div(d->tokens, kChunkLong), kJoinChunks) * slabs >= kMostGroups / 2) return DQGAN_EINVAL;
     return DQGAN_OK;
 }
 

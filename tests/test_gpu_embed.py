@@ -203,3 +203,36 @@ def test_tokens_of_very_many_places(D, dt):
         want = torch.zeros((V, D)).index_add_(0, tok[m][keep], dout[m][keep].float()) * 0.5
         assert torch.equal(G[m, :V * D].view(V, D).cpu(), want), m
     plan.close()
+
+
+def test_most_tokens():
+    """2^30 tokens of one worker, all but some of whose gradients are 0, which add
+    nothing to a sum."""
+    import torch
+    from paper_2010_13359_amd import layers
+    N, V = 2 ** 30, 5
+    pl = ref.plan(V, 1)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    P = torch.randn((1, pl.ld), generator=g, device="cuda")
+    tok = torch.randint(-1, V, (1, N), generator=g, device="cuda", dtype=torch.int32)
+    x = torch.empty((1, N, 1), dtype=torch.float16, device="cuda")
+    print("lookup", flush=True)
+    layers.embed_forward(pl, tok, P, x, V, scale=2.0)
+    part = 2 ** 27
+    for a in range(0, N, part):
+        t = tok[0, a:a + part].long()
+        want = torch.where(t >= 0, 2.0 * P[0, t.clamp(min=0)], 0.0).half()
+        assert torch.equal(x[0, a:a + part, 0], want), a
+    del t, want
+    at = torch.randint(0, N, (5000,), generator=g, device="cuda").unique()
+    at = torch.cat([at, torch.tensor([0, N - 1], device="cuda")]).unique()
+    x.zero_()
+    x[0, at, 0] = torch.randn(at.numel(), generator=g, device="cuda").half()
+    G = torch.full((1, pl.ld), 7.0, device="cuda")
+    ws = layers.embed_workspace(pl, N, V, 1, x.dtype, tok.dtype)
+    print("gradient", flush=True)
+    layers.embed_backward(pl, tok, x, G, V, ws, scale=0.5)
+    w = ref.embed_backward(tok[0, at], x[0, at], V, 0.5)
+    ref.check("G", G[0, :V].view(V, 1), w[0], w[1])
+    assert bool((G[0, V:] == 7.0).all())
+    pl.close()

@@ -156,3 +156,18 @@ def test_header_is_plain_c(tmp_path):
                         "-Wl,-rpath," + pkg + ":/opt/rocm/lib"], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout + r.stderr
     assert subprocess.run([str(tmp_path / "uses")], timeout=100).returncode == 0
+
+
+@pytest.mark.parametrize("kind,size", [(0, 4), (1, 2), (2, 2)])
+def test_most_tokens(lib, kind, size):
+    """Every number of tokens that the header allows, at widths whose activations stay
+    below a terabyte: a workspace is named, and its size is that of two pairs of lists
+    and two partial sums for every 32 tokens."""
+    p, n = FakePlan(M=1), ctypes.c_size_t()
+    for tokens, width in ((2 ** 30, 1), (2 ** 30, 2 ** 10 // size), (2 ** 29 + 1, 1), (2 ** 29 + 1, 2 ** 11 // size - 1),
+                          (2 ** 21, 2 ** 19 // size - 1)):
+        p = FakePlan(d=3 * width + 10, M=1)
+        d = ctypes.byref(_embed(tokens=tokens, width=width, vocab=3, type=kind))
+        assert lib.dqgan_embed_bytes(p.handle, d, ctypes.byref(n)) == 0, (tokens, width)
+        lists = 4 * ((4 * tokens + 255) // 256 * 256)
+        assert n.value == lists + 4 * 2 * ((tokens + 31) // 32) * width, (tokens, width)
