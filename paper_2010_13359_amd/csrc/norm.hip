@@ -488,13 +488,14 @@ int64_t forward_groups(int64_t M, int64_t N, int rows_per_group, int threads) {
 // 32 of 512 9.0 and 12.3, 8 of 5000 13.3 and 15.8; with 16 turns 64 rows of 1024 would
 // take 18 where shares take 12, 16 of 5000 24 and 16.
 constexpr int64_t kAlone = 8;
-// Otherwise 8 rows at least, and 4 of those that take a workgroup each while there
-// are CUs for all (1000 rows of 4096 f16 14.7 us and 18.2, 500 of 12288 19.7 and 26.2;
-// 2 x 1000 of 12288 52 and 43).
+// Otherwise 8 rows at least (16 where a workgroup takes as many at a time), and 4 of
+// those that take a workgroup each while there are CUs for all (1000 rows of 4096 f16
+// 14.7 us and 18.2, 500 of 12288 19.7 and 26.2; 2 x 1000 of 12288 52 and 43).
 int shares_of(int64_t M, int64_t N, int groups, int least, int rows, int threads) {
     if (ceil_div(N, rows) <= kAlone) return 1;
+    const int few = rows > 8 ? rows : 8;
     const bool short_ones = rows == 1 && M * ceil_div(N, 4) <= (threads > 256 ? 256 : 512);
-    const int64_t want = ceil_div(groups, M), most = ceil_div(N, short_ones ? 4 : M * N < 8192 ? 8 : least);
+    const int64_t want = ceil_div(groups, M), most = ceil_div(N, short_ones ? 4 : M * N < 8192 ? few : least);
     const int64_t s = most < want ? most : want;
     return static_cast<int>(s < 1 ? 1 : s);
 }

@@ -171,3 +171,17 @@ def test_most_tokens(lib, kind, size):
         assert lib.dqgan_embed_bytes(p.handle, d, ctypes.byref(n)) == 0, (tokens, width)
         lists = 4 * ((4 * tokens + 255) // 256 * 256)
         assert n.value == lists + 4 * 2 * ((tokens + 31) // 32) * width, (tokens, width)
+
+
+@pytest.mark.parametrize("M", [1, 3, 32, 200])
+@pytest.mark.parametrize("width", [1, 31, 64, 128])
+def test_norm_shares_have_rows(lib, width, M):
+    """Rows of up to 16 lanes are taken 16 at a time: a worker's sums are kept apart in
+    no more shares than that makes, and in one without a workspace up to 128 rows."""
+    n = ctypes.c_size_t()
+    for tokens in list(range(1, 700)) + [1000, 4001, 8191, 8192, 70001]:
+        d = ctypes.byref(_norm(tokens=tokens, width=width, gamma=0, beta=width + 4))
+        assert lib.dqgan_norm_bytes(FakePlan(M=M).handle, d, ctypes.byref(n)) == 0
+        shares = n.value // (4 * 2 * width * M)
+        assert n.value == shares * 4 * 2 * width * M
+        assert (shares == 0) == (tokens <= 128) and shares <= (tokens + 15) // 16, (tokens, shares)
