@@ -40,6 +40,27 @@ def check(name, got, want, err):
             name, int(bad.sum()), bad.numel(), i, float(got[i]), float(want[i]), float(b)))
 
 
+def check_range(name, got, want, err):
+    """check, with what lies beyond the type's range: a value is an infinity of its sign
+    from half a step above the largest one on (a tie, whose even neighbour is the one that
+    is not there); where `err` reaches across that edge, it is that infinity or finite.
+    Returns how many have to be infinities."""
+    info = torch.finfo(got.dtype)
+    edge = info.max + 2.0 ** math.floor(math.log2(info.max)) * info.eps / 2
+    got, want = got.detach().double().cpu(), want.double().cpu()
+    err = err.double().cpu() if isinstance(err, torch.Tensor) else torch.full_like(want, err)
+    infinite = torch.copysign(torch.full_like(want, math.inf), want)
+    over = (want.abs() - err >= edge) | torch.isinf(want)
+    near = (want.abs() + err >= edge) & ~over
+    assert bool((got == infinite)[over].all()), "%s: not infinite" % name
+    assert bool(torch.isnan(got[torch.isnan(want)]).all()), "%s: not NaN" % name
+    half = info.eps / 2
+    bound = err + half * (want.abs() + err) + info.smallest_normal * half
+    good = ((got - want).abs() <= bound) | (near & (got == infinite)) | over | torch.isnan(want)
+    assert bool(good.all()), "%s: beyond the bound at %s" % (name, (~good).nonzero()[:3].tolist())
+    return int(over.sum())
+
+
 def depth(D):
     """Additions on the way of one term into a row's sum: at most 8 per vector
     and lane, 6 across lanes, 16 across waves."""
@@ -197,4 +218,83 @@ def distill(z, val, idx, weight, V, T):
         g_err.index_add_(0, i, t_err + k * U * t)
         out["dz"][n, :V] = w[n] * T * g
         out["dz_err"][n, :V] = w[n].abs() * T * (g_err + 4 * U * (s + (s - g).abs()))
+    return out
+
+
+def _additions(V, size):
+    """Additions on the way of one exponential into its row's sum: a lane's vectors in
+    registers and LDS, one single element, 6 across a wave and up to 4 across waves;
+    and of a row in slices, those of a slice, then the slices of a lane and 8 more."""
+    per, bytes_ = 16 // size, V * size
+    for most, vectors in ((4096, 1), (8192, 2), (16384, 4), (32768, 8), (65536, 16), (131072, 16), (196608, 12), (261120, 16)):
+        if bytes_ <= most:
+            row = per * vectors + 1 + 6 + 4
+            break
+    else:
+        row = 0
+    slices = per * 4 + 1 + 6 + 2 + math.ceil(math.ceil(bytes_ / 16384) / 256) + 8
+    return max(row, slices)
+
+
+def distill_close(z, val, idx, weight, V, T):
+    """As distill, with what the kernels' own steps may be off by and no more.
+
+    x = (z - largest) / T: the difference's own rounding, taken as it is, and, if T is
+    no power of two, two more.  exp(x) of 32-bit logits: 2 u of the exponential and one
+    rounding (the product with log2(e) is corrected); of 16-bit ones u |x| each for
+    log2(e) / T and the product, and 2 u.  A row in slices has one more exponential and a
+    product for each slice."""
+    dtype, size = z.dtype, z.element_size()
+    fine = dtype == torch.float32
+    z, val = z.detach().cpu(), val.detach().cpu()
+    N, ld, k = z.shape[0], z.shape[1], val.shape[1]
+    idx = idx.cpu().long() & 0xFFFFFFFF
+    w = torch.ones(N, dtype=torch.float64) if weight is None else weight.double().cpu()
+    inv = 0.0 if math.frexp(T)[0] == 0.5 else 2 * U
+    adds, adds_k = _additions(V, size), math.ceil(k / 256) + 10
+    out = {n: torch.zeros(N, dtype=torch.float64) for n in ("loss", "loss_err", "largest", "total", "total_err")}
+    out["dz"], out["dz_err"] = (torch.zeros((N, ld), dtype=torch.float64) for _ in range(2))
+
+    def exponent(a, top):
+        """(a - top) / T and its error."""
+        d32 = (a.float() - top.float()).double()
+        d = a.double() - top.double()
+        return d / T, (d32 - d).abs() / T + inv * d.abs() / T
+    for n in range(N):
+        use = (idx[n] < V) & ~(val[n] == -math.inf)
+        if w[n] == 0 or not bool(use.any()):
+            continue
+        v, i = val[n][use], idx[n][use]
+        top = z[n, :V].max()
+        x, x_err = exponent(z[n, :V], top)
+        e = x.exp()
+        total = e.sum()
+        e_rel = x_err + (3 * U if fine else 2 * U * (1 + x.abs()))
+        slice_rel = (U * 3 if fine else U * (2 + 2 * float(x.abs().max()))) + U if V * size > 131072 else 0.0
+        total_rel = float((e_rel * e).sum() / total) + slice_rel + adds * U
+        s = e / total
+        s_err = s * (e_rel + total_rel + 2 * U)
+        av, av_err = exponent(v, v.max())
+        ev = av.exp()
+        sum_v = ev.sum()
+        t = ev / sum_v
+        sum_rel = float(((av_err + 2 * U) * t).sum()) + adds_k * U
+        t_err = t * (av_err + 3 * U + sum_rel)
+        logt = av - sum_v.log()
+        logs = x[i] - total.log()
+        gap = (logt - logs).abs()
+        logt_err = av_err + sum_rel + 2 * U * sum_v.log().abs() + U * logt.abs()
+        logs_err = x_err[i] + total_rel + 2 * U * total.log().abs() + U * logs.abs()
+        term = t * (logt - logs)
+        term_err = t_err * gap + t * (logt_err + logs_err + U * gap)
+        out["loss"][n] = w[n] * T * T * term.sum()
+        out["loss_err"][n] = w[n].abs() * T * T * (term_err.sum() + (adds_k + 3) * U * term.abs().sum()) * 1.001
+        out["largest"][n], out["total"][n], out["total_err"][n] = top, total, total * total_rel * 1.001
+        times = torch.bincount(i, minlength=V).double()
+        g, g_err = s.clone(), s_err.clone()
+        g.index_add_(0, i, -t)
+        g_err.index_add_(0, i, t_err + U * t * times[i])
+        g_err += torch.where(times > 0, U * g.abs(), 0.0)
+        out["dz"][n, :V] = w[n] * T * g
+        out["dz_err"][n, :V] = w[n].abs() * T * (g_err + 2 * U * g.abs()) * 1.001
     return out

@@ -211,3 +211,39 @@ def test_gradient_against_differences():
     third = 8 * float(E.abs().max()) ** 3 * float(weight.sum()) / T
     assert abs(float((hi - lo) / (2 * h) - mine)) <= h * h * third / 6 + 2e-5 * float(size)
     pl.close()
+
+
+def _compare_closely(z, val, idx, weight, V, T, got):
+    loss, stats, dz = got
+    for m in range(z.shape[0]):
+        w = ref.distill_close(z[m], val[m], idx[m], None if weight is None else weight[m], V, T)
+        ref.check("largest", stats[m, :, 0], w["largest"], 0.0)
+        ref.check("total", stats[m, :, 1], w["total"], w["total_err"])
+        ref.check("loss", loss[m], w["loss"], w["loss_err"])
+        ref.check_range("dz", dz[m], w["dz"], w["dz_err"])
+
+
+@pytest.mark.parametrize("dt", sorted(ref.TYPES))
+@pytest.mark.parametrize("shape", SHAPES)
+def test_no_further_off_than_the_kernels_steps(shape, dt):
+    V = shape[2]
+    for T, spread in ((1.0, 3.0), (2.0, 12.0), (2.5, 8.0)):
+        pl, z, val, idx, weight = _setup(shape, dt, seed=V + 1, spread=spread)
+        _compare_closely(z, val, idx, weight, V, T, _run(pl, z, val, idx, weight, V, T))
+        pl.close()
+
+
+@pytest.mark.parametrize("V", [3, 200, 1001])
+def test_small_probabilities_keep_their_digits(V):
+    """Logits on a grid, so that their differences are exact: an exponential of 2^-100
+    is off by 3 u in 32 bits, and would be by 40 u without the correction of its
+    exponent's product."""
+    import torch
+    pl, z, val, idx, weight = _setup((1, 8, V, 0, 2), "f32", seed=7)
+    gen = torch.Generator().manual_seed(V)
+    z[..., :V] = -torch.randint(0, 80 * 256, (1, 8, V), generator=gen).cuda() / 256.0
+    z[..., 0] = 0.0
+    idx[..., 0], idx[..., 1] = 0, 1
+    for T in (1.0, 0.5):
+        _compare_closely(z * T, val, idx, weight, V, T, _run(pl, z * T, val, idx, weight, V, T))
+    pl.close()
