@@ -415,3 +415,43 @@ def test_widest_rows():
         layers.embed_forward(plan, tok[:, :1], P, torch.empty((1, 1, D + 1), device="cuda"), 1)
     assert e.value.status == dqgan.EINVAL
     plan.close()
+
+
+# ---------------------------------------------------------------------------
+# beyond the type
+
+
+@pytest.mark.parametrize("dt,big", [("f16", 1e4)])
+@pytest.mark.parametrize("D", [5, 64, 131, 700])
+def test_beyond_the_type(dt, big, D):
+    """Results above the type's largest value are infinities of their sign, whole vectors
+    and single elements alike, and their neighbours stay as they are.  (bf16 ends where
+    binary32 does: what is beyond it is beyond the sums that it is made of.)"""
+    import torch
+    from paper_2010_13359_amd import layers
+    M, N, V, k = 1, 12, 40, 3
+    gen = torch.Generator().manual_seed(D)
+    pl = ref.plan(V * D, M)
+    dtype = ref.TYPES[dt]
+    P = (big * torch.randn((M, pl.ld), generator=gen) ** 3).cuda()
+    tok = torch.randint(0, V, (M, N), generator=gen).cuda()
+    x = torch.empty((M, N, D), dtype=dtype, device="cuda")
+    layers.embed_forward(pl, tok, P, x, V, scale=2.0)
+    w = ref.embed_forward(tok[0], P[0, :V * D].view(V, D), 2.0)
+    assert ref.check_range("lookup", x[0], w[0], w[1]) > 0
+    x.copy_(torch.randn((M, N, D), generator=gen))
+    y, stats, dx = torch.empty_like(x), torch.empty((M, N, 2), device="cuda"), torch.empty_like(x)
+    layers.norm_forward(pl, x, P, y, stats, gamma=0, beta=2 * D, eps=1e-3)
+    w = ref.norm_forward(x[0], P[0, :D], P[0, 2 * D:3 * D], 1e-3)
+    assert ref.check_range("y", y[0], w[0], w[1]) > 0
+    dy = (3 * torch.randn((M, N, D), generator=gen)).to(dtype).cuda()
+    layers.norm_backward(pl, x, dy, P, stats, dx, P.clone(), layers.norm_workspace(pl, N, D, dtype, 0, 2 * D), 0, 2 * D)
+    w = ref.norm_backward(x[0], dy[0], P[0, :D], stats[0])
+    assert ref.check_range("dx", dx[0], w[0], w[1]) > 0
+    z = (20 * torch.randn((M, N, D), generator=gen)).to(dtype).cuda()
+    val, idx = torch.randn((M, N, k), generator=gen).cuda(), torch.randint(0, D, (M, N, k), generator=gen).int().cuda()
+    weight, loss, dz = torch.full((M, N), 50 * big, device="cuda"), torch.empty((M, N), device="cuda"), torch.empty_like(z)
+    layers.distill_fused(pl, z, val, idx, weight, loss, dz, D)
+    w = ref.distill_close(z[0], val[0], idx[0], weight[0], D, 1.0)
+    assert ref.check_range("dz", dz[0], w["dz"], w["dz_err"]) > 0
+    pl.close()
