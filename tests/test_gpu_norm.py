@@ -207,3 +207,11 @@ def test_a_large_mean_costs_no_digits(D, dt, kind):
     ref.check("mean", stats[0, :, 0], w[2], w[3])
     ref.check("rstd", stats[0, :, 1], w[4], w[5])
     pl.close()
+
+
+@pytest.mark.parametrize("dt", sorted(ref.TYPES))
+@pytest.mark.parametrize("D", [320, 321, 832, 833, 1600, 1601, 3328, 3329, 6400, 6401, 9216, 9217])
+def test_the_other_row_shapes(D, dt):
+    """Widths on both sides of the row shapes that the lists above leave out."""
+    test_forward(D, dt)
+    test_backward(D, dt)
