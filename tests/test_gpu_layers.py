@@ -455,3 +455,41 @@ def test_beyond_the_type(dt, big, D):
     w = ref.distill_close(z[0], val[0], idx[0], weight[0], D, 1.0)
     assert ref.check_range("dz", dz[0], w["dz"], w["dz_err"]) > 0
     pl.close()
+
+
+@pytest.mark.parametrize("kind,extra", [("identity", {}), ("sign", {}), ("qsgd", {"levels": 15}), ("topk", {"keep": 300}),
+                                        ("mbit", {"levels": 8, "norm": "linf"})])
+def test_every_iteration_of_the_student(kind, extra, monkeypatch):
+    """What the compressor takes in every iteration is written whole (G is NaN before), at
+    evaluation points that the last iteration moved, and the losses are those of 64 bits
+    there.  (The gradients themselves: test_students_gradients.)"""
+    import torch
+    from paper_2010_13359_amd import closed_loop
+    real, points = closed_loop.Student.gradients, []
+
+    def gradients(self, P, tokens, val, idx, weight, G):
+        d = self.parameters(self.vocab, self.width)[0]
+        G[:, :d] = float("nan")
+        loss = real(self, P, tokens, val, idx, weight, G)
+        assert bool(torch.isfinite(G[:, :d]).all()) and bool(G[:, :d].any(1).all())
+        assert not points or not torch.equal(points[-1], P)
+        points.append(P.clone())
+        V, D = self.vocab, self.width
+        for m in range(P.shape[0]):
+            E, beta = P[m, :V * D].double().view(V, D), P[m, V * D + D:d].double()
+            x = E[tokens[m]] * self.scale
+            xc = x - x.mean(-1, keepdim=True)
+            y = xc / ((xc * xc).mean(-1, keepdim=True) + 1e-5).sqrt() * P[m, V * D:V * D + D].double() + beta
+            s = torch.log_softmax(y @ E.T / self.temperature, -1)
+            t = torch.log_softmax(val[m].double() / self.temperature, -1)
+            T2 = self.temperature ** 2
+            want = weight[m].double() * T2 * (t.exp() * (t - s.gather(-1, idx[m].long()))).sum(-1)
+            # a logit of D terms is off by D u of their sizes and by y's own error, up to 2 depth(D) u of
+            # it; it comes twice into the loss, as itself and in the sum, and t (log t - log s), below 10
+            # here, is off by some 20 u of itself
+            off = (D + 2 * ref.depth(D)) * ref.U * (y.abs() @ E.abs().T).amax(-1)
+            assert bool(((loss[m].double() - want).abs() <= weight[m] * T2 * (4 * off + 200 * ref.U)).all())
+        return loss
+    monkeypatch.setattr(closed_loop.Student, "gradients", gradients)
+    hist = closed_loop.run_student(kind, T=4, **extra)
+    assert len(hist) == 4 == len(points)
