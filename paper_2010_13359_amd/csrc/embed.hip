@@ -835,7 +835,8 @@ dqgan_status dqgan_embed_backward(dqgan_plan P, const dqgan_embed_desc *d, const
             constexpr int L = decltype(l)::value, C = decltype(c)::value;
             const dim3 grid(static_cast<uint32_t>(ceil_div(chunks * slabs, 256 / L)), my);
             with_stream(backward_streams(static_cast<double>(sizeof(T)) * M * a.N * a.D), [&](auto streams) {
-                k_embed_sum<T, L, C, decltype(streams)::value><<<grid, 256, 0, st>>>(
+                // short chunks are of 34 MB of dout at most
+                k_embed_sum<T, L, C, decltype(streams)::value && C == kChunkLong><<<grid, 256, 0, st>>>(
                     key[now], at[now], static_cast<const T *>(dout), a, chunks, slabs, width, part, G, add != 0);
             });
             if (chunks > 2)

@@ -134,7 +134,7 @@ struct Centre {
 // left.  Bound by memory: 8 x
 // 8192 rows of 2048 bf16 (537 MB) 95 us, 5.7 TB/s of the 6.1 of a large copy; few
 // rows are one launch and two sums over a wave, 2.7 us.
-template <typename T, typename S, int STREAM>
+template <typename T, typename S, bool STREAM>
 __global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a, T *y, float *stats) {
     constexpr int kPer = Vec16<T>::kPer, NV = S::kVectors;
     typedef typename Vec16<T>::wide Wide;
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a
     for (int64_t first = S::first_row(); first < a.N; first += step) {
         const bool in = first + S::row_of_wave() < a.N;
         const int64_t n = in ? first + S::row_of_wave() : a.N - 1;
-        Row<T, S, (STREAM > 1)> row;
+        Row<T, S, false> row;
         row.load(x + (m * a.N + n) * D, lane, vectors, rest);
         Wide f[NV];
         float last = lane < rest ? widen_bits<T>(row.last) : 0.0f, s = last;
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_fwd(const T *x, NormArgs a
             const int q = lane + S::kLanes * v;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) f[v][i] = fmaf(centre.normal(f[v][i]), g.of[v][i], b.of[v][i]);
-            if (q < vectors && in) store16<T, (STREAM > 0)>(at(out, kPer * q), narrow<T>(f[v]));
+            if (q < vectors && in) store16<T, STREAM>(at(out, kPer * q), narrow<T>(f[v]));
         }
         if (lane < rest && in) *at(out, kPer * vectors + lane) = static_cast<T>(fmaf(centre.normal(last), g.last, b.last));
         if (stats && lane == 0 && in) {
@@ -500,11 +500,12 @@ int shares_of(int64_t M, int64_t N, int groups, int least, int rows, int threads
     return static_cast<int>(s < 1 ? 1 : s);
 }
 
-// How the rows pass by the caches, by the bytes of all of them: 0 not, 1 what is
-// written, 2 what is read too.  Forward, 8192 rows of 2048 bf16 for each of 8
-// workers (537 MB): 95.6 us written so, 107.5 not; 66 MB the same.  Backward, f32,
-// 1611 MB: 307 us not, 299 written so, 274 both; bf16, 98 MB: 25.4, 22.3 and 24.9.
-int forward_streams(double bytes) { return bytes > 100e6 ? 1 : 0; }
+// How the rows pass by the caches, by the bytes of all of them.  Forward: whether what
+// is written does; 8192 rows of 2048 bf16 for each of 8 workers (537 MB): 95.6 us
+// written so, 107.5 not; 66 MB the same.  Backward: 0 not, 1 what is written, 2 what is
+// read too; f32, 1611 MB: 307 us not, 299 written so, 274 both; bf16, 98 MB: 25.4, 22.3
+// and 24.9.
+bool forward_streams(double bytes) { return bytes > 100e6; }
 int backward_streams(double bytes) { return bytes > 200e6 ? 2 : bytes > 80e6 ? 1 : 0; }
 template <typename F>
 void with_streams(int streams, F &&f) {
@@ -599,9 +600,9 @@ dqgan_status dqgan_norm_forward(dqgan_plan P, const dqgan_norm_desc *d, const vo
                 using S = decltype(s);
                 const dim3 grid(static_cast<uint32_t>(forward_groups(M, d->tokens, S::kRows, S::kThreads)), my);
                 if (forward_streams(2.0 * sizeof(T) * M * d->tokens * d->width))
-                    k_norm_fwd<T, S, 1><<<grid, S::kThreads, 0, st>>>(from, a, to, stats);
+                    k_norm_fwd<T, S, true><<<grid, S::kThreads, 0, st>>>(from, a, to, stats);
                 else
-                    k_norm_fwd<T, S, 0><<<grid, S::kThreads, 0, st>>>(from, a, to, stats);
+                    k_norm_fwd<T, S, false><<<grid, S::kThreads, 0, st>>>(from, a, to, stats);
             }))
             k_norm_fwd_long<T><<<dim3(static_cast<uint32_t>(forward_groups(M, d->tokens, 1, 1024)), my), 1024, 0, st>>>(
                 from, a, to, stats);
