@@ -704,11 +704,18 @@ void with_index(int32_t type, F &&f) {
         f(int64_t{});
 }
 
-// Whether `out` passes by the caches: 134 MB 47 us so and 53 not, 33 MB 13.4 and
-// 15.7 (rows of 501 bf16: 15.1 and 14.1), 17 MB the same.  Not narrow rows with
-// single channels behind the last four, whose lines come in many pieces: 1.6 million
-// of 35 f32 127 us and 90, 1.2 million of 71 bf16 145 and 128, of 117 156 and 153.
-bool forward_streams(double bytes, int64_t D) { return bytes > 30e6 && (D % 4 == 0 || D >= 100); }
+// Whether `out` passes by the caches.  Rows of whole vectors from 30 MB on: 134 MB of
+// 1024 bf16 47 us so and 53 not, 40 MB 14.4 and 15.5, of 64 11.9 and 12.5; 20 MB the
+// same.  The lines of other rows come in pieces, from vectors and single channels:
+// from 60 MB on (40 MB of 138 bf16 20.2 and 17.8, 60 MB 26.9 and 29.2, of 203 f32 14.3
+// and 13.5, 19.2 and 21.3) if they have 256 bytes (800 MB: 138 bf16 363 and 366, 71 f32
+// 338 and 341, but 57 f32 430 and 298, 71 bf16 542 and 479), or from 65 to 160 MB, about
+// what the Infinity Cache takes, if they have 140 (71 bf16: 60 MB 37 and 34, 80 MB 47
+// and 54, 150 MB 95 and 102, 220 MB 159 and 143; 117: 70 MB 32 and 36).
+bool forward_streams(double bytes, int64_t D, int64_t size) {
+    if (D % 4 == 0) return bytes > 30e6;
+    return D * size >= 256 ? bytes > 60e6 : D * size >= 140 && bytes > 65e6 && bytes < 160e6;
+}
 // Whether dout passes by the caches: 268 MB 148 us (the whole gradient) so and 181
 // not, 134 MB 356 and 365, 33 MB 118 and 114.
 bool backward_streams(double bytes) { return bytes > 100e6; }
@@ -753,7 +760,7 @@ dqgan_status dqgan_embed_forward(dqgan_plan P, const dqgan_embed_desc *d, const 
             using I = decltype(i);
             const int64_t groups = ceil_div(a.N, forward_rows<T> * (256 >> shift));
             const dim3 grid(static_cast<uint32_t>(groups < 65536 ? groups : 65536), static_cast<uint32_t>(P->desc.M));
-            if (forward_streams(static_cast<double>(sizeof(T)) * P->desc.M * a.N * a.D, a.D))
+            if (forward_streams(static_cast<double>(sizeof(T)) * P->desc.M * a.N * a.D, a.D, sizeof(T)))
                 k_embed_fwd<T, I, true><<<grid, 256, 0, st>>>(static_cast<const I *>(tok), params, ldp, a, shift, vectors,
                                                               static_cast<T *>(out));
             else

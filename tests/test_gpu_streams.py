@@ -176,11 +176,12 @@ def test_norm(dt, shape):
 
 
 # ---------------------------------------------------------------------------
-# embedding: the lookup's results pass by the caches above 30 MB (narrow odd rows not),
+# embedding: the lookup's results pass by the caches above 30 MB, rows with single
+# channels above 60 MB if they have 256 bytes, between 65 and 160 MB if they have 140;
 # the gradient's rows above 100 MB.
 
 
-@pytest.mark.parametrize("D", [64, 99, 130, 1027])
+@pytest.mark.parametrize("D", [31, 64, 99, 130, 1027])
 @pytest.mark.parametrize("dt", sorted(ref.TYPES))
 def test_lookup(dt, D):
     import torch
@@ -189,7 +190,7 @@ def test_lookup(dt, D):
     pl = ref.plan(V * D + 7, M)
     g = torch.Generator(device="cuda").manual_seed(D)
     P = torch.randn((M, pl.ld), generator=g, device="cuda")
-    for bytes_ in (28e6, 34e6):
+    for bytes_ in (28e6, 34e6, 65e6, 90e6, 170e6):
         N = int(bytes_ / (M * D * size))
         tok = torch.randint(-1, V + 1, (M, N), generator=g, device="cuda")
         out = torch.full((M, N, D), float("nan"), dtype=dtype, device="cuda")
