@@ -18,9 +18,14 @@ struct DistillArgs {
 
 constexpr float kNone = -INFINITY;
 
-// exp((z - largest) / T) as a power of two.  A 32-bit result carries along what
-// the rounding of the exponent's product with log2(e) lost: at an exponent of
-// 2^6 that is up to 3e-6 of the result.  A 16-bit result has no use for it.
+// exp(x), x = (z - largest) / T, as a power of two.  Of 32-bit logits it carries along
+// what the rounding of the exponent's product with log2(e) lost: at an exponent of 2^6
+// that is up to 3e-6 of the result.  Of 16-bit logits it does not: the constant and the
+// product are off by 2 |x| 2^-24 of the result.  dz has 16 bits and no use for more.  The
+// statistics and the loss have 32: their sum is off by the softmax's mean of that, at
+// most 2 ln(V) 2^-24 (the mean of |x| is the softmax's entropy less the logarithm of the
+// sum, which is 1 or more), 1.4e-6 for 128000 logits that were themselves rounded to
+// 2^-12 or 2^-9.
 template <bool FINE>
 __device__ __forceinline__ float exp_of(const DistillArgs &a, float z, float largest) {
     if (!FINE) return __builtin_amdgcn_exp2f((z - largest) * a.log2e_T);
@@ -332,6 +337,9 @@ __global__ __launch_bounds__(64 * W, NV == kTwoVectors ? 8 : 1) void k_distill_r
         const float coef = weight * a.T, over = coef / x.total;
         l.gradient(a, x.largest, over, to, vectors, rest, held);
         clear<T, W>(to, a.V, a.ld);
+        // Entries come after their vectors, streamed ones too: stores of a workgroup's
+        // waves to one address stay in the order that a barrier gives them, as they
+        // leave through one compute unit's cache.
         __syncthreads();
         for (int j = tid; j < a.k; j += 64 * W)
             if (s.idx[j] != UINT32_MAX) to[s.idx[j]] = static_cast<T>(entry_gradient<FINE>(a, s, have, x, coef, j));
@@ -460,8 +468,7 @@ void with_shape(int64_t bytes, F &&f) {
 //    none: loss and gradient of 64 rows of 128000 bf16 logits 15 us in slices and
 //    21 by rows, of 128 rows of 80000 16 and 18, of 256 26 and 22.
 // The rule does not ask whether the gradient is wanted too, so that the loss has the
-// same bits with it and without (slices would be faster for the loss alone of 4096
-// rows of 128000: 197 us and 250).
+// same bits with it and without.
 bool split(int64_t rows, int64_t bytes) { return bytes > kRowMost || (bytes > kRowFewer && rows <= kFewRows); }
 int64_t slices_of(int64_t bytes) { return ceil_div(bytes, 64 * 4 * kSliceVectors * 16); }
 

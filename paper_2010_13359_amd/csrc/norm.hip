@@ -267,7 +267,7 @@ struct Sums {
 // its columns' sums of dy and dy * xh in registers meanwhile: x and dy are read once
 // for all three results.  8 x
 // 2048 rows of 1024 bf16 (101 MB) 20.8 us, and k_norm_params 3.9; 3 x 1111 rows of
-// 4801 f16 (96 MB, and 20 MB of sums) 27.5 and 5.1: a row's two sums over the
+// 4801 f16 (96 MB, and 16 MB of sums written and read) 27.5 and 5.1: a row's two sums over the
 // workgroup come between its loads and its stores, and loads of the next row ahead
 // of them were no faster.
 template <typename T, typename S, int STREAM>
@@ -473,7 +473,9 @@ __global__ __launch_bounds__(1024) void k_norm_params(const float *part, int sha
 
 // ---------------------------------------------------------------------------
 
-constexpr int kForwardMost = 32768, kBackwardMost = 16384;  // widest rows that stay in registers
+// Widest rows that stay in registers; forward, of f32 they are those of up to 17408,
+// which 16 waves of four vectors hold.
+constexpr int kForwardMost = 32768, kBackwardMost = 16384;
 
 // Workgroups per worker of the forward pass: 8192 in all, and 2048 of wide rows,
 // whose weight and bias are as much to read as a row (8192 and 2048: rows of 2048
@@ -503,8 +505,10 @@ int shares_of(int64_t M, int64_t N, int groups, int least, int rows, int threads
 // How the rows pass by the caches, by the bytes of all of them.  Forward: whether what
 // is written does; 8192 rows of 2048 bf16 for each of 8 workers (537 MB): 95.6 us
 // written so, 107.5 not; 66 MB the same.  Backward: 0 not, 1 what is written, 2 what is
-// read too; f32, 1611 MB: 307 us not, 299 written so, 274 both; bf16, 98 MB: 25.4, 22.3
-// and 24.9.
+// read too.  Rows of 1024 bf16, us with 0, 1 and 2: 50 MB 15.8 15.9 18.1, 90 MB 23.4
+// 21.7 24.1, 130 MB 32.6 28.9 30.4, 220 MB 55.8 54.4 51.8, 800 MB 158.6 156.9 143.9; of
+// f32 22.8 20.5 22.6 with 90 MB and 48.5 47.4 44.9 with 220; rows of 512 to 9000 in the
+// same order (9000 bf16: all three within 2 % from 130 MB on; 180 MB of 1024: 2 by 4 %).
 bool forward_streams(double bytes) { return bytes > 100e6; }
 int backward_streams(double bytes) { return bytes > 200e6 ? 2 : bytes > 80e6 ? 1 : 0; }
 template <typename F>
