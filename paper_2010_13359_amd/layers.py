@@ -68,10 +68,10 @@ def load():
     return L
 
 
-def _type(dtype, name):
-    t = TYPES.get(dtype)
+def _type(dtype, name, types=TYPES):
+    t = types.get(dtype)
     if t is None:
-        raise TypeError("%s: dtype %s, expected one of %s" % (name, dtype, ", ".join(str(t) for t in TYPES)))
+        raise TypeError("%s: dtype %s, expected one of %s" % (name, dtype, ", ".join(str(t) for t in types)))
     return t
 
 
@@ -177,7 +177,7 @@ def embed_forward(plan, tokens, P, out, vocab, offset=0, scale=1.0, stream=None)
 def embed_workspace(plan, tokens, vocab, width, dtype, index_dtype=torch.int64, offset=0):
     """A workspace for embed_backward with `tokens` tokens per worker."""
     return _new(plan, _desc(plan, EmbedDesc, "dqgan_embed_bytes", offset, vocab, width, tokens, 1.0,
-                            _type(dtype, "dtype"), INDEX_TYPES[index_dtype], 0)[1])
+                            _type(dtype, "dtype"), _type(index_dtype, "index_dtype", INDEX_TYPES), 0)[1])
 
 
 def embed_backward(plan, tokens, dout, G, vocab, workspace, offset=0, scale=1.0, add=False, stream=None):

@@ -185,3 +185,15 @@ def test_norm_shares_have_rows(lib, width, M):
         shares = n.value // (4 * 2 * width * M)
         assert n.value == shares * 4 * 2 * width * M
         assert (shares == 0) == (tokens <= 128) and shares <= (tokens + 15) // 16, (tokens, shares)
+
+
+def test_workspaces_of_other_types_are_refused():
+    """By the same error as tensors of other types, with the names of those that are taken."""
+    import torch
+    from paper_2010_13359_amd import layers
+    for call in (lambda: layers.embed_workspace(None, 300, 50, 20, torch.float32, torch.int16),
+                 lambda: layers.embed_workspace(None, 300, 50, 20, torch.float64),
+                 lambda: layers.norm_workspace(None, 300, 20, torch.int32),
+                 lambda: layers.distill_workspace(None, 300, 50, 20, torch.float64)):
+        with pytest.raises(TypeError, match="expected one of"):
+            call()
