@@ -112,8 +112,8 @@ struct Params {
 // 0.05.  Such rows (the mean above eight deviations) take the mean r of x - mean too,
 // and y and the variance about mean + r: off by 1e-7 and 3e-7.  Of the others y is off
 // by at most 8 (depth of the sum) 2^-24 for it, and they cost one comparison (8 x 4000
-// rows of 9000 bf16, one in a hundred of them far, 262 us; without r 254, with r for
-// all rows 279; 32 x 16384 of 64 29, 28 and 31).
+// rows of 9000 bf16 262 us; without r 254, with r for all rows 279; 32 x 16384 of 64
+// with one row in a hundred far 29, 28 and 31, with none 26.9 and 26.1).
 constexpr float kFar = 64.0f;  // the square of eight
 struct Centre {
     float var, rstd, r = 0.0f, shift = 0.0f;

@@ -5,7 +5,8 @@ and whose parameter gradients go into the rows of the gradients.
 
 As in ``dqgan``, torch tensors supply device memory and the stream, and every
 tensor is checked against the plan and the other tensors before the call;
-outputs and workspaces are the caller's.  Activations are float32, bfloat16 or
+outputs and workspaces are the caller's.  The calls leave no autograd graph: each
+operator's gradient is a call of its own.  Activations are float32, bfloat16 or
 float16, ``[M][tokens][width]`` and contiguous.
 """
 import ctypes
